@@ -305,7 +305,7 @@ typedef struct ssd_rows {
  *   state [nslots, H, P, N] fp32: the slots of the plan's sequences are read (carry) and replaced, the others left as they are
  *   ws    ssd_packed_workspace_bytes() bytes (0: bad arguments), 256-byte aligned
  * States and fp32 outputs are fp32 results in every dtype; cumulative sums of dt A are kept in 64 bits.  bf16 y: the masked scores and the
- * state in front of 128 rows are rounded once to bf16 as operands, 2^-8 of each of their terms, as the result is; D x is added in fp32.
+ * state in front of 128 rows are operands of two bf16 parts, 2^-16 of each of their terms; D x is added in fp32, and the result rounded once.
  * A plan may cut a long sequence into ranges of whole 128 rows, whose states are then joined from sums: the bits of a result depend on the
  * plan, not on other calls or on what ws holds, and repeat.  A value that is not finite stays in its sequence, in its row's block of 128
  * rows and what follows.  Calls that share ws, on one stream or in graphs, run one after the other; ws is used from the first launch to

@@ -918,15 +918,17 @@ namespace {
 bool heads_by_twos(int64_t units, int heads) { return units * heads > kNumSMs; }
 
 // Ranges that the sequences are cut into, so that a batch of few or uneven sequences keeps all SMs busy.  Cutting costs a launch for the sums, so
-// the number is the one with the least estimated time, CTAs the longest first on 148 SMs.  With blocks of 128 rows of one head (bf16) as items,
-// a CTA's time in us is 5 + 2.3 items and 0.8 for each range in front, whose states it reads, a CTA's for the sums 4.7 + 1.1 items: fitted to 182
-// runs of 13 batches with 1 to 32 ranges, 6% off on the average.  One B200, us, the batch with one range, with the estimate's number, with the best:
-//   one of 49153 rows, 64 heads     862   610   604      9000 + 15 of 300, 24 heads   293    95    93
-//   one of 131072 rows, 80 heads   2276  1878  1878      four of 1000, 24 heads        30    30    30
-//   one of 2048 rows, 24 heads       48    28    28      six of 50 to 3000, 8 heads    52    32    32
-//   three of 4096 rows, 80 heads    143   143   143      30 of 100 to 6000, 32 heads  341   341   341
-// fp32 takes ten times as long in much the same proportions (one of 16384 rows, 24 heads 3183, 747, 747), but for short sequences, where a CTA's
-// start weighs less: seven of 17 to 510 rows of 4 heads 103, 103, 43.  A plan does not know the type.
+// the number is the one with the least estimated time, CTAs the longest first on 148 SMs.  With blocks of 128 rows of one head (bf16, N = 128) as
+// items, a CTA's time in us is 5 + 2.3 items and 0.8 for each range in front, whose states it reads, a CTA's for the sums 4.7 + 1.1 items: fitted to 182
+// runs of 13 batches with 1 to 32 ranges, 6% off on the average, when operands of one part each made an item 2.3 us; with two parts it is 2.65, which
+// changes none of the choices below.  One B200, us, the batch with one range, with the estimate's number, with the best:
+//   one of 49153 rows, 64 heads     999   667   667      9000 + 15 of 300, 24 heads   351   103   101
+//   one of 131072 rows, 80 heads   2639  2116  2116      four of 1000, 24 heads        34    34    34
+//   one of 2048 rows, 24 heads       53    31    30      six of 50 to 3000, 8 heads    58    34    34
+//   three of 4096 rows, 80 heads    168   168   168      30 of 100 to 6000, 32 heads  400   400   400
+//   one of 16384 rows, 24 heads, N = 64   302   104   102
+// fp32 takes ten times as long in much the same proportions (one of 16384 rows, 24 heads 3191, 750, 750), but for short sequences, where a CTA's
+// start weighs less: seven of 17 to 510 rows of 4 heads 106, 106, 43.  A plan does not know the type.
 int ranges_of(int64_t n, int rows) { return n > rows ? (int)((n + rows - 1) / rows) : 1; }
 // rows of range r of m of a sequence of n: equal parts in blocks
 void range_at(int64_t n, int m, int r, int64_t &begin, int64_t &end) {

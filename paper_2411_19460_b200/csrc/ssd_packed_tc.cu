@@ -10,24 +10,25 @@
 // with the row's factor in it, on the diagonal element by element.  From the first row on instead of from the middle, half the decay was the
 // limit, and heads that passed it took a quarter longer, a whole batch with them.
 //
-// What is rounded: X' to three bf16 parts (nothing is lost: the states are fp32 results).  M and H to one: 2^-8 of each of their terms in y,
-// which is itself rounded to 2^-8; D x is added in fp32.  Sums are fp32 in tensor memory.  cs is summed in 64 bits and kept as two fp32 numbers:
-// with strong decays it runs into the thousands.
+// What is rounded: X' to three bf16 parts (nothing is lost: the states are fp32 results).  M and H to two, 2^-16 of each of their terms in y, which
+// is itself rounded to 2^-8; D x is added in fp32.  One part of each, 2^-8 of its terms, costs y 40% more error than its own rounding where the products
+// are all of it (D = 0), and nothing where D x is most of it: 24 prompts took 305 us so, the second part of M 26 more, that of H 22 (now 342).
+// Sums are fp32 in tensor memory.  cs is summed in 64 bits and kept as two fp32 numbers: with strong decays it runs into the thousands.
 //
 // Products (cycles of the tensor pipe): G 512 a block; S 1150 (one part after the other onto the same sums, N = 64, which 48 cycles of reading
-// shared memory bound; side by side, 768, they take 128 columns more and the states three times the loads), C H 400, M X 256 (M from tensor
-// memory) an item.  Columns of tensor memory: G 128, M two times 64, M X 64, C H 64, S 64.
+// shared memory bound; side by side, 768, they take 128 columns more and the states three times the loads), C H 770, M X 512 (M from tensor
+// memory) an item.  Columns of tensor memory: G 128, M two halves of 64 steps times 64, M X 64, C H two times 64 in turn, S 64.
 //
-// Warps, meeting only through mbarriers (tests/test_packed_roles.py has a model of who waits for what):
+// Warps, meeting only through mbarriers (tests/test_packed_halves.py and test_packed_roles.py have a model of who waits for what):
 //   0 G and M X   1 S and C H   2, 3 decays of even and odd items   4..11 parts of x'   12..15 outputs   16..23 mask, but for one without
 //   a sub-tile: loads   24..31 states, half of p each four
-// Bound by the roles' latency and the hand-overs between them: 3600 cycles an item (two heads), of which the longest roles take 2300 (mask), 2000
-// (parts of x'), 1600 (outputs) and the tensor pipe 2060.  24 prompts, 23760 tokens, of 80 heads: 270 us (2.4 TB/s; its bytes alone 93 us), three of
-// 4096 146 us, one of 49153 of 64 heads 610 with its sums.  What it took: y over x and parts of x' in a ring of three times 32 steps instead of
-// twice 64, so that four items' x fit instead of two, and x ahead of C (4250 -> 3600 cycles an item); factors of the mask from the middle row (5200
-// -> 3900 for strong decays, then); short code, for the roles' loops together go through the instruction cache once per item (79, 69, 57 KB: 358,
-// 310, 291 us).  Taken back, slower or no faster: scores ahead of M X, or what of the two is ready first; C H behind the next item's S; y by warps;
-// the next block prefetched into L2; polls that sleep or stay.
+// Bound by shared memory: 4150 cycles an item (two heads), in which the products' operands take 2430 at 128 bytes a cycle, the parts of x' 510, the
+// states' 260, outputs 260 and the copies in and out 500, and the tensor pipe 2690.  24 prompts, 23760 tokens, of 80 heads: 342 us (1.8 TB/s; its bytes
+// alone 93 us), three of 4096 168 us, one of 49153 of 64 heads with 8 groups 786 with its sums (a pass among others).  What it took: y over x and parts of x'
+// in a ring of three times 32 steps instead of twice 64, and x ahead of C; factors of the mask from the middle row (for strong decays); short code, for
+// the roles' loops together go through the instruction cache once per item; with two parts of M and H, C H in two places and the halves of M one by one (353
+// -> 342).  Four items' x instead of three made no difference.  Taken back, slower or no faster: scores ahead of M X, or what of the two is ready first;
+// C H behind the next item's S; y by warps; the next block prefetched into L2; polls that sleep or stay; sums given back ahead of the last stores.
 #include "ssd_internal.h"
 #include "ssd_packed.h"
 #include "ssd_split.cuh"
@@ -44,14 +45,14 @@ static_assert(PT_R_ISSUE + PT_R_OUT + 2 * PT_R_X + 2 * PT_R_MASK + 2 * PT_R_STAT
 
 constexpr int PT_SLOTS = 3;                             // ring of B and C tiles, in turn
 constexpr int PT_VECS = 3;                              // ring of the items' decays
-constexpr int PT_XS = 4;                                // ring of the items' rows of x, in whose place y goes
+constexpr int PT_XS = 3;                                // ring of the items' rows of x, in whose place y goes
 constexpr int PT_PARTS = 3;                             // ring of the parts of x' of 32 steps
 // per item: weights of x' | e^{cs_t} | the output's factor of M X | column factors of the row sub-tiles 0 .. 3 (32, 64, 96, 128 columns) |
 // cs, first and second part | dt | e^{cs_last}
 enum { PV_W = 0, PV_E = 128, PV_R = 256, PV_F = 384, PV_HI = 704, PV_LO = 832, PV_DT = 960, PV_DECAY = 1088, PV_FLOATS = 1120 };
 template <int N> struct PtMem {
     static constexpr uint32_t TILE = 128 * N * 2;
-    static constexpr uint32_t X = PT_SLOTS * TILE < 65536 ? 65536 : PT_SLOTS * TILE, XP = X + PT_XS * 16384, H = XP + PT_PARTS * 12288, VEC = H + N * 128;
+    static constexpr uint32_t X = PT_SLOTS * TILE < 65536 ? 65536 : PT_SLOTS * TILE, XP = X + PT_XS * 16384, H = XP + PT_PARTS * 12288, VEC = H + 2 * N * 128;
     static constexpr uint32_t BYTES = VEC + PT_VECS * PV_FLOATS * 4;
 };
 static_assert(PtMem<128>::BYTES <= 232448 - 1024, "shared memory");
@@ -108,7 +109,8 @@ __device__ __forceinline__ void pt_wait_watched(uint64_t *bar, uint32_t parity, 
             break;
         }
 }
-// A role's place in the ring of the decays: slot, and whether its pass over the ring is an odd one
+// A role's place in a ring of three (decays, parts of x'): slot, and whether its pass over the ring is an odd one
+static_assert(PT_PARTS == PT_VECS, "rings of one length");
 struct VecTurn {
     uint32_t slot = 0, odd = 0;
     __device__ __forceinline__ void next(uint32_t by = 1) {
@@ -126,6 +128,12 @@ __device__ __forceinline__ uint32_t pt_pack(float a, float b) {
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 __device__ __forceinline__ float2 pt_unpack(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+// Two bf16 parts of two values: rounded, and what that leaves out, rounded (2^-16 of the value at most)
+__device__ __forceinline__ void pt_pack2(float a, float b, uint32_t &w, uint32_t &r) {
+    w = pt_pack(a, b);
+    const float2 f = pt_unpack(w);
+    r = pt_pack(a - f.x, b - f.y);
+}
 // Products and their hand-over by one thread (`on`) of a warp that runs its loop together: in a branch of that thread alone every descriptor
 // took two more instructions.  `acc` 0: the first of a sum.
 __device__ __forceinline__ void pt_mma(uint32_t on, uint32_t acc, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc) {
@@ -167,11 +175,11 @@ k_packed_tc(PackedParams p, const __grid_constant__ CUtensorMap tmX, const __gri
             const __grid_constant__ CUtensorMap tmY) {
     using Mem = PtMem<N>;
     constexpr int KN = N / 16;                          // steps of a contraction over n
-    constexpr uint32_t TM_G = 0, TM_M = 128, TM_Y = 256, TM_CH = 320, TM_S = 384;
+    constexpr uint32_t TM_G = 0, TM_M = 128, TM_Y = 256, TM_CH = 320, TM_S = 448;
     extern __shared__ __align__(1024) unsigned char smem[];          // swizzled tiles start on multiples of 1024
     __shared__ uint64_t tfull[PT_SLOTS], tempty[PT_SLOTS], xfull[PT_XS], xempty[PT_XS], xready[PT_XS];
     __shared__ uint64_t vfull[PT_VECS], vempty[PT_VECS];
-    __shared__ uint64_t gfull, gfree, mfull[2], mempty[2], xpfull[PT_PARTS], xpempty[PT_PARTS], sdone, sfree, hfull, chdone, yfull, yfree, tailtx, tailfull, alldone;
+    __shared__ uint64_t gfull, gfree, mfull[2], mempty[2], xpfull[PT_PARTS], xpempty[PT_PARTS], sdone, sfree, hfull, chdone[2], chfree[2], yfull, yfree, tailtx, tailfull, alldone;
     __shared__ uint32_t tmem_base, abort_flag;
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -183,6 +191,8 @@ k_packed_tc(PackedParams p, const __grid_constant__ CUtensorMap tmX, const __gri
         for (int i = 0; i < 2; ++i) {
             mbar_init(&mempty[i], 1);
             mbar_init(&mfull[i], 7);
+            mbar_init(&chdone[i], 1);
+            mbar_init(&chfree[i], 4);
         }
         for (int i = 0; i < PT_VECS; ++i) {
             mbar_init(&vfull[i], 1);
@@ -202,7 +212,6 @@ k_packed_tc(PackedParams p, const __grid_constant__ CUtensorMap tmX, const __gri
         mbar_init(&sdone, 1);
         mbar_init(&sfree, N / 16);
         mbar_init(&hfull, N / 16);
-        mbar_init(&chdone, 1);
         mbar_init(&yfull, 1);
         mbar_init(&yfree, 4);
         mbar_init(&tailtx, 2);
@@ -249,14 +258,18 @@ k_packed_tc(PackedParams p, const __grid_constant__ CUtensorMap tmX, const __gri
                     if (i >= 0) {
                         pt_wait(&xready[i % PT_XS], (i / PT_XS) & 1, abortp);
                         if (i) pt_wait(&yfree, (i - 1) & 1, abortp);
-                        pt_wait(&mfull[i & 1], (i >> 1) & 1, abortp);
-                        tc_fence_after_sync();
-                        const uint32_t lX = loM + Mem::X / 16 + (i % PT_XS) * 1024, lM = tm + TM_M + (i & 1) * 64;
+                        // 64 steps at a time, as their masks get ready; the smaller part first
+#pragma unroll 1
+                        for (int side = 0; side < 2; ++side) {
+                            const uint32_t lX = loM + Mem::X / 16 + (i % PT_XS) * 1024 + side * 512, lM = tm + TM_M + side * 64;
+                            pt_wait(&mfull[side], i & 1, abortp);
+                            tc_fence_after_sync();
 #pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            pt_mma_ta(on, k, tm + TM_Y, lM + 8 * k, umma_desc_words(lX + k * 128, hiM), idY);
+                            for (int n = 0; n < 8; ++n)
+                                pt_mma_ta(on, side + n, tm + TM_Y, lM + (n < 4 ? 32 : 0) + 8 * (n & 3), umma_desc_words(lX + (n & 3) * 128, hiM), idY);
+                            pt_commit(on, &mempty[side]);
+                        }
                         pt_commit(on, &yfull);
-                        pt_commit(on, &mempty[i & 1]);
                     }
                     if (j == nh - 1 && c + 1 < nb) {                 // the next block's scores
                         const int kb = 2 * c + 2, kc = kb + 1;
@@ -307,14 +320,14 @@ k_packed_tc(PackedParams p, const __grid_constant__ CUtensorMap tmX, const __gri
                 if constexpr (!SUMS) {
                     if (j == 0) wait_tile(kc);
                     pt_wait(&hfull, i & 1, abortp);
-                    if (i) pt_wait(&yfree, (i - 1) & 1, abortp);
+                    if (i >= 2) pt_wait(&chfree[i & 1], ((i >> 1) - 1) & 1, abortp);
                     tc_fence_after_sync();
 #pragma unroll
-                    for (int k = 0; k < KN; ++k) {
-                        const uint32_t o = (k >> 2) * 1024 + (k & 3) * 2;
-                        pt_mma(on, k, tm + TM_CH, umma_desc_words(lC + o, hiK), umma_desc_words(lH + k * 128, hiM), idC);
+                    for (int n = 0; n < 2 * KN; ++n) {               // the smaller part first
+                        const uint32_t k = n % KN, o = (k >> 2) * 1024 + (k & 3) * 2;
+                        pt_mma(on, n, tm + TM_CH + 64 * (i & 1), umma_desc_words(lC + o, hiK), umma_desc_words(lH + (n < KN ? N * 8 : 0) + k * 128, hiM), idC);
                     }
-                    pt_commit(on, &chdone);
+                    pt_commit(on, &chdone[i & 1]);
                     if (j == nh - 1) pt_commit(on, &tempty[kc % PT_SLOTS]);
                 }
                 if (++j == nh) {
@@ -455,14 +468,14 @@ k_packed_tc(PackedParams p, const __grid_constant__ CUtensorMap tmX, const __gri
             if (lane == 0) mbar_arrive(&vempty[vt.slot]);
             unsigned char *xs = smem + Mem::X + (i % PT_XS) * 16384;
             const float2 e2 = make_float2(et, et), r2 = make_float2(rt, rt), D2 = make_float2(Dh, Dh);
-            pt_wait(&chdone, i & 1, abortp);
+            pt_wait(&chdone[i & 1], (i >> 1) & 1, abortp);
             pt_wait(&yfull, i & 1, abortp);              // so x has been read by all others: by the product, which came behind its parts
             tc_fence_after_sync();
 #pragma unroll 1
             for (int k = 0; k < 4; ++k) {
                 float a[16], b[16];
                 uint4 xv[2];
-                tmem_ld16_nowait(tl + TM_CH + 16 * k, a);
+                tmem_ld16_nowait(tl + TM_CH + 64 * (i & 1) + 16 * k, a);
                 tmem_ld16_nowait(tl + TM_Y + 16 * k, b);
 #pragma unroll
                 for (int n = 0; n < 2; ++n) xv[n] = *reinterpret_cast<const uint4 *>(xs + r * 128 + (((2 * k + n) ^ (r & 7)) << 4));
@@ -485,7 +498,7 @@ k_packed_tc(PackedParams p, const __grid_constant__ CUtensorMap tmX, const __gri
             tc_fence_before_sync();
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&yfree);
+            if (lane == 0) mbar_arrive(&yfree), mbar_arrive(&chfree[i & 1]);
             asm volatile("bar.sync 1, 128;" ::: "memory");
             const int left = u.n - c * 128, row = u.row0 + c * 128;
             if (left >= 128) {
@@ -516,8 +529,8 @@ k_packed_tc(PackedParams p, const __grid_constant__ CUtensorMap tmX, const __gri
             for (int m = 0; m < 16; ++m) z[m] = 0u;
             for (int k = half; k < 4; k += 2)
                 if (k > q) {                                         // above the diagonal, for good
-                    tmem_st16(tl + TM_M + 16 * k, z);
-                    tmem_st16(tl + TM_M + 64 + 16 * k, z);
+                    tmem_st16(tl + TM_M + 64 * (k >> 1) + 16 * half, z);
+                    tmem_st16(tl + TM_M + 64 * (k >> 1) + 16 * half + 32, z);
                 }
             tmem_st_wait();
             tc_fence_before_sync();
@@ -564,57 +577,63 @@ k_packed_tc(PackedParams p, const __grid_constant__ CUtensorMap tmX, const __gri
                 const float *F = v + PV_F + 16 * q * (q + 1);        // column factors of row sub-tile q
                 if (j == 0) pt_wait(&gfull, c & 1, abortp);
                 tc_fence_after_sync();
-                if (i >= 2) pt_wait(&mempty[i & 1], ((i >> 1) - 1) & 1, abortp);
-                const uint32_t tM = tl + TM_M + (i & 1) * 64;
-                // 16 columns at a time, both of a sub-tile, then two sub-tiles on
+                // a sub-tile of each half of the columns, 16 at a time
 #pragma unroll 1
-                for (int k = 2 * half; k < 2 * q + 2; k += k & 1 ? 3 : 1) {
-                    float a[16];
-                    __syncwarp();
-                    tmem_ld16(tl + TM_G + 16 * k, a);
-                    if (mild) {
+                for (int side = 0; side < 2; ++side) {
+                    const int sub = 2 * side + half;
+                    if (i) pt_wait(&mempty[side], (i - 1) & 1, abortp);
+                    tc_fence_after_sync();
+#pragma unroll 1
+                    for (int k = 2 * sub; k < 2 * sub + 2 && sub <= q; ++k) {
+                        const uint32_t to = tl + TM_M + 64 * side + 8 * (k & 3);
+                        float a[16];
+                        __syncwarp();
+                        tmem_ld16(tl + TM_G + 16 * k, a);
+                        if (mild) {
 #pragma unroll
-                        for (int m = 0; m < 16; m += 4) {
-                            const float4 f = *reinterpret_cast<const float4 *>(F + 16 * k + m);
-                            const float2 x0 = __fmul2_rn(make_float2(a[m], a[m + 1]), make_float2(f.x, f.y));
-                            const float2 x1 = __fmul2_rn(make_float2(a[m + 2], a[m + 3]), make_float2(f.z, f.w));
-                            a[m] = x0.x; a[m + 1] = x0.y; a[m + 2] = x1.x; a[m + 3] = x1.y;
-                        }
-                    } else {                                         // with the row's factor, on the diagonal element by element
-                        const float hi = v[PV_HI + t], lo = v[PV_LO + t];
-                        const float rf = pt_ex2((hi - v[PV_HI + q * 32]) + (lo - v[PV_LO + q * 32]));
-#pragma unroll
-                        for (int m = 0; m < 16; m += 4) {
-                            const int s = 16 * k + m;
-                            float4 f;
-                            if (k < 2 * q) {
-                                f = *reinterpret_cast<const float4 *>(F + s);
-                                f.x *= rf, f.y *= rf, f.z *= rf, f.w *= rf;
-                            } else {
-                                const float4 sh = *reinterpret_cast<const float4 *>(v + PV_HI + s), sl = *reinterpret_cast<const float4 *>(v + PV_LO + s);
-                                f = *reinterpret_cast<const float4 *>(v + PV_DT + s);
-                                f.x *= pt_ex2((hi - sh.x) + (lo - sl.x)), f.y *= pt_ex2((hi - sh.y) + (lo - sl.y));
-                                f.z *= pt_ex2((hi - sh.z) + (lo - sl.z)), f.w *= pt_ex2((hi - sh.w) + (lo - sl.w));
+                            for (int m = 0; m < 16; m += 4) {
+                                const float4 f = *reinterpret_cast<const float4 *>(F + 16 * k + m);
+                                const float2 x0 = __fmul2_rn(make_float2(a[m], a[m + 1]), make_float2(f.x, f.y));
+                                const float2 x1 = __fmul2_rn(make_float2(a[m + 2], a[m + 3]), make_float2(f.z, f.w));
+                                a[m] = x0.x; a[m + 1] = x0.y; a[m + 2] = x1.x; a[m + 3] = x1.y;
                             }
-                            a[m] *= f.x, a[m + 1] *= f.y, a[m + 2] *= f.z, a[m + 3] *= f.w;
+                        } else {                                         // with the row's factor, on the diagonal element by element
+                            const float hi = v[PV_HI + t], lo = v[PV_LO + t];
+                            const float rf = pt_ex2((hi - v[PV_HI + q * 32]) + (lo - v[PV_LO + q * 32]));
+#pragma unroll
+                            for (int m = 0; m < 16; m += 4) {
+                                const int s = 16 * k + m;
+                                float4 f;
+                                if (k < 2 * q) {
+                                    f = *reinterpret_cast<const float4 *>(F + s);
+                                    f.x *= rf, f.y *= rf, f.z *= rf, f.w *= rf;
+                                } else {
+                                    const float4 sh = *reinterpret_cast<const float4 *>(v + PV_HI + s), sl = *reinterpret_cast<const float4 *>(v + PV_LO + s);
+                                    f = *reinterpret_cast<const float4 *>(v + PV_DT + s);
+                                    f.x *= pt_ex2((hi - sh.x) + (lo - sl.x)), f.y *= pt_ex2((hi - sh.y) + (lo - sl.y));
+                                    f.z *= pt_ex2((hi - sh.z) + (lo - sl.z)), f.w *= pt_ex2((hi - sh.w) + (lo - sl.w));
+                                }
+                                a[m] *= f.x, a[m + 1] *= f.y, a[m + 2] *= f.z, a[m + 3] *= f.w;
+                            }
                         }
-                    }
-                    if (k >= 2 * q) {
+                        if (k >= 2 * q) {
 #pragma unroll
-                        for (int m = 0; m < 16; ++m) a[m] = 16 * k + m <= t ? a[m] : 0.f;
-                    }
-                    uint32_t o[8];
+                            for (int m = 0; m < 16; ++m) a[m] = 16 * k + m <= t ? a[m] : 0.f;
+                        }
+                        uint32_t o[8], r[8];
 #pragma unroll
-                    for (int m = 0; m < 8; ++m) o[m] = pt_pack(a[2 * m], a[2 * m + 1]);
+                        for (int m = 0; m < 8; ++m) pt_pack2(a[2 * m], a[2 * m + 1], o[m], r[m]);
+                        __syncwarp();
+                        tmem_st8(to, o);
+                        tmem_st8(to + 32, r);
+                    }
+                    tmem_st_wait();
+                    tc_fence_before_sync();
                     __syncwarp();
-                    tmem_st8(tM + 8 * k, o);
+                    if (lane == 0) mbar_arrive(&mfull[side]);
                 }
-                tmem_st_wait();
-                tc_fence_before_sync();
-                __syncwarp();
                 if (lane == 0) {
                     if (j == nh - 1) mbar_arrive(&gfree);
-                    mbar_arrive(&mfull[i & 1]);
                     mbar_arrive(&vempty[vt.slot]);
                 }
                 if (++j == nh) {
@@ -660,13 +679,15 @@ k_packed_tc(PackedParams p, const __grid_constant__ CUtensorMap tmX, const __gri
             VecTurn vt;
             auto step = [&](float (&s)[32], double &dl, int i) {
                 if constexpr (!SUMS) {
-                    if (i) pt_wait(&chdone, (i - 1) & 1, abortp);        // the state of the item before has been read
+                    if (i) pt_wait(&chdone[(i - 1) & 1], ((i - 1) >> 1) & 1, abortp);        // the state of the item before has been read
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        uint32_t w[4];
+                        uint32_t w[4], r[4];
 #pragma unroll
-                        for (int m = 0; m < 4; ++m) w[m] = pt_pack(s[8 * k + 2 * m], s[8 * k + 2 * m + 1]);
-                        *reinterpret_cast<uint4 *>(hp + (((4 * half + k) ^ (n & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        for (int m = 0; m < 4; ++m) pt_pack2(s[8 * k + 2 * m], s[8 * k + 2 * m + 1], w[m], r[m]);
+                        unsigned char *to = hp + (((4 * half + k) ^ (n & 7)) << 4);
+                        *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4 *>(to + N * 128) = make_uint4(r[0], r[1], r[2], r[3]);
                     }
                     fence_proxy_async_smem();
                     __syncwarp();
