@@ -3,15 +3,17 @@
 // through ctypes its host side took 15 us per call and set the pace of a generation loop.
 //
 // Every function takes positional arguments (None where the Python wrapper has None), launches on the given stream or,
-// for None, on the current one, and returns its tensors; a negative SSD_* code of the library comes back as an int, for
+// for None, on the current one, where its own allocations belong too (CallStream), and returns its tensors; a negative SSD_* code of the library comes back as an int, for
 // the wrapper to raise.
 #include <ATen/ATen.h>
 #include <Python.h>
+#include <ATen/ops/record_stream.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <optional>
 #include <vector>
 
 #include "ssd.h"
@@ -36,15 +38,42 @@ long long num(PyObject *o) {
     if (v == -1 && PyErr_Occurred()) throw python_error();
     return v;
 }
-void *stream_of(PyObject *o) {
-    if (o == Py_None) return (void *)c10::cuda::getCurrentCUDAStream().stream();
-    PyObject *v = PyObject_GetAttrString(o, "cuda_stream");
-    if (!v) throw python_error();
-    void *p = PyLong_AsVoidPtr(v);
-    Py_DECREF(v);
-    if (!p && PyErr_Occurred()) throw python_error();
-    return p;
-}
+// The stream that a call launches on: the given one, or the current one of the device of `ref`.  While the call runs it is the current one, so that
+// what the call allocates, copies and fills is its stream's: scratch that is freed at return is handed out again behind the call's own work, not beside
+// it, and nothing writes a result whose memory another stream still works on.
+struct CallStream {
+    void *st = nullptr;
+    CallStream(PyObject *o, const at::Tensor &ref) {
+        if (ref.is_cuda()) device_.reset_device(ref.device());
+        const c10::cuda::CUDAStream now = c10::cuda::getCurrentCUDAStream();
+        st = (void *)now.stream();
+        if (o == Py_None) return;
+        PyObject *v = PyObject_GetAttrString(o, "cuda_stream");
+        if (!v) throw python_error();
+        void *p = PyLong_AsVoidPtr(v);
+        Py_DECREF(v);
+        if (!p && PyErr_Occurred()) throw python_error();
+        if (p == st) return;
+        st = p;
+        was_ = now;
+        on_ = c10::cuda::getStreamFromExternal((cudaStream_t)p, now.device_index());
+        stream_.reset_stream(*on_);
+    }
+    // A new result: its memory is not handed out again either before work that the caller's current stream has by then is done
+    at::Tensor result(at::Tensor t) const {
+        if (was_) t.record_stream(*was_);
+        return t;
+    }
+    // A tensor of the call's caller that may be dropped while the work still reads it
+    void uses(const at::Tensor &t) const {
+        if (on_ && t.is_cuda()) t.record_stream(*on_);
+    }
+
+private:
+    c10::cuda::OptionalCUDAGuard device_;
+    c10::cuda::OptionalCUDAStreamGuard stream_;
+    std::optional<c10::cuda::CUDAStream> was_, on_;
+};
 int dtype_code(const at::Tensor &t, const char *msg) {
     if (t.scalar_type() == at::kBFloat16) return SSD_DTYPE_BF16;
     if (t.scalar_type() == at::kFloat) return SSD_DTYPE_F32;
@@ -57,8 +86,8 @@ at::Tensor f32_like(const at::Tensor &ref, at::IntArrayRef sizes) { return at::e
 at::Tensor bytes(const at::Tensor &ref, size_t n) { return at::empty({(int64_t)n}, ref.options().dtype(at::kByte)); }
 size_t nbytes(const at::Tensor &ws) { return (size_t)ws.numel() * ws.element_size(); }
 // the caller's tensor as it is, or a new one
-template <typename F> PyObject *given_or(PyObject *o, F make) {
-    if (o == Py_None) return THPVariable_Wrap(make());
+template <typename F> PyObject *given_or(const CallStream &on, PyObject *o, F make) {
+    if (o == Py_None) return THPVariable_Wrap(on.result(make()));
     tensor(o);
     Py_INCREF(o);
     return o;
@@ -110,6 +139,7 @@ PyObject *decode_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
         at::Tensor x = tensor(a[0]), dt = tensor(a[1]), Bm = tensor(a[3]), Cm = tensor(a[4]);
         const at::Tensor &h = tensor(a[6]);
         require(x.is_cuda() && h.is_cuda(), PyExc_ValueError, "device tensors required");
+        const CallStream on(a[8], x);
         static const char *const kToken = "ssd_decode_step takes one token: x [B,1,H,P], dt [B,1,H], Bm/Cm [B,1,G,N]";
         require(x.dim() == 4 && Bm.dim() == 4, PyExc_ValueError, kToken);
         const int64_t B = x.size(0), H = x.size(2), P = x.size(3), G = Bm.size(2), N = Bm.size(3);
@@ -128,13 +158,13 @@ PyObject *decode_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
         if (!Bm.is_contiguous()) Bm = Bm.contiguous();
         if (!Cm.is_contiguous()) Cm = Cm.contiguous();
         Results out;
-        PyObject *y = out.add(given_or(a[7], [&] { return at::empty({B, 1, H, P}, x.options()); }));
+        PyObject *y = out.add(given_or(on, a[7], [&] { return at::empty({B, 1, H, P}, x.options()); }));
         const at::Tensor &yt = tensor(y);
         require(yt.is_contiguous() && yt.sizes() == x.sizes() && yt.scalar_type() == x.scalar_type(), PyExc_ValueError,
                 "y must be a dense tensor like x");
         ssd_shape_t s = {(int32_t)B, 1, (int32_t)H, (int32_t)P, (int32_t)N, (int32_t)G, 0, 0, code, 0, 0, 0, 0};
         const int rc = unlocked(ssd_decode_step, &s, x.data_ptr(), (const float *)dt.data_ptr(), fptr(a[2]), Bm.data_ptr(), Cm.data_ptr(), fptr(a[5]),
-                                       (float *)h.data_ptr(), yt.data_ptr(), stream_of(a[8]));
+                                       (float *)h.data_ptr(), yt.data_ptr(), on.st);
         if (rc) return PyLong_FromLong(rc);
         Py_INCREF(y);
         return y;
@@ -168,19 +198,20 @@ PyObject *fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const ssd_shape_t s = layer_shape(a, a[7], a[8], a[9]);
         const bool seg = a[12] != Py_False;
         const at::Tensor &x = tensor(a[0]);
+        const CallStream on(a[14], x);
         Results out;
-        PyObject *y = out.add(given_or(a[10], [&] { return at::empty_like(x); }));
-        PyObject *hf = out.add(given_or(a[11], [&] { return f32_like(x, {s.B, s.H, s.P, s.N}); }));
+        PyObject *y = out.add(given_or(on, a[10], [&] { return at::empty_like(x); }));
+        PyObject *hf = out.add(given_or(on, a[11], [&] { return f32_like(x, {s.B, s.H, s.P, s.N}); }));
         PyObject *bd = nullptr;
         if (seg) {
             const size_t nb = a[12] == Py_None ? ssd_boundary_bytes(&s) : 1;
             if (!nb) return PyLong_FromLong(SSD_EINVAL);
-            bd = out.add(given_or(a[12], [&] { return f32_like(x, {s.B, (int64_t)(nb / (4ull * s.B * s.H * s.P * s.N)), s.H, s.P, s.N}); }));
+            bd = out.add(given_or(on, a[12], [&] { return f32_like(x, {s.B, (int64_t)(nb / (4ull * s.B * s.H * s.P * s.N)), s.H, s.P, s.N}); }));
         }
         const size_t need = a[13] == Py_None ? ssd_workspace_bytes(&s, seg ? SSD_OP_FWD_SEG : SSD_OP_FWD) : 1;
         if (!need) return PyLong_FromLong(SSD_EINVAL);
         const at::Tensor ws = a[13] == Py_None ? bytes(x, need) : tensor(a[13]);
-        void *st = stream_of(a[14]);
+        void *st = on.st;
         const int rc = seg ? unlocked(ssd_fwd_segmented, &s, x.data_ptr(), fptr(a[1]), fptr(a[2]), ptr(a[3]), ptr(a[4]), fptr(a[5]), fptr(a[6]), ptr(y), fptr(hf),
                                                fptr(bd), ws.data_ptr(), nbytes(ws), st)
                            : unlocked(ssd_fwd, &s, x.data_ptr(), fptr(a[1]), fptr(a[2]), ptr(a[3]), ptr(a[4]), fptr(a[5]), fptr(a[6]), ptr(y), fptr(hf),
@@ -195,12 +226,13 @@ PyObject *bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded(n, 21, [&]() -> PyObject * {
         const ssd_shape_t s = layer_shape(a, a[9], a[10], a[11]);
         const at::Tensor &x = tensor(a[0]);
+        const CallStream on(a[20], x);
         const size_t need = a[19] == Py_None ? ssd_workspace_bytes(&s, SSD_OP_BWD_SEG) : 1;
         if (!need) return PyLong_FromLong(SSD_EINVAL);
         const at::Tensor ws = a[19] == Py_None ? bytes(x, need) : tensor(a[19]);
         return PyLong_FromLong(unlocked(ssd_bwd_segmented, &s, x.data_ptr(), fptr(a[1]), fptr(a[2]), ptr(a[3]), ptr(a[4]), fptr(a[5]), fptr(a[6]), ptr(a[7]),
                                                  fptr(a[8]), ptr(a[12]), fptr(a[13]), fptr(a[14]), ptr(a[15]), ptr(a[16]), fptr(a[17]), fptr(a[18]),
-                                                 ws.data_ptr(), nbytes(ws), stream_of(a[20])));
+                                                 ws.data_ptr(), nbytes(ws), on.st));
     });
 }
 
@@ -220,10 +252,11 @@ PyObject *conv_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded(n, 7, [&]() -> PyObject * {
         const at::Tensor &u = tensor(a[0]);
         const ConvArgs c = conv_args(u);
+        const CallStream on(a[6], u);
         Results out;
-        PyObject *o = out.add(given_or(a[4], [&] { return at::empty_like(u); }));
-        PyObject *so = out.add(given_or(a[5], [&] { return at::empty({c.B, 3, c.C}, u.options()); }));
-        const int rc = unlocked(ssd_conv_fwd, c.B, c.L, c.C, c.code, u.data_ptr(), c.bs, fptr(a[1]), fptr(a[2]), ptr(a[3]), ptr(o), ptr(so), stream_of(a[6]));
+        PyObject *o = out.add(given_or(on, a[4], [&] { return at::empty_like(u); }));
+        PyObject *so = out.add(given_or(on, a[5], [&] { return at::empty({c.B, 3, c.C}, u.options()); }));
+        const int rc = unlocked(ssd_conv_fwd, c.B, c.L, c.C, c.code, u.data_ptr(), c.bs, fptr(a[1]), fptr(a[2]), ptr(a[3]), ptr(o), ptr(so), on.st);
         if (rc) return PyLong_FromLong(rc);
         return out.tuple();
     });
@@ -234,15 +267,16 @@ PyObject *conv_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded(n, 13, [&]() -> PyObject * {
         const at::Tensor &u = tensor(a[0]);
         const ConvArgs c = conv_args(u);
+        const CallStream on(a[12], u);
         const auto f32 = u.options().dtype(at::kFloat);
         Results out;
-        PyObject *du = out.add(given_or(a[6], [&] { return at::empty_like(u); }));
-        PyObject *ds = out.add(given_or(a[7], [&] { return at::empty({c.B, 3, c.C}, f32); }));
-        PyObject *dw = out.add(given_or(a[8], [&] { return at::zeros({c.C, 4}, f32); }));
-        PyObject *db = out.add(given_or(a[9], [&] { return at::zeros({c.C}, f32); }));
+        PyObject *du = out.add(given_or(on, a[6], [&] { return at::empty_like(u); }));
+        PyObject *ds = out.add(given_or(on, a[7], [&] { return at::empty({c.B, 3, c.C}, f32); }));
+        PyObject *dw = out.add(given_or(on, a[8], [&] { return at::zeros({c.C, 4}, f32); }));
+        PyObject *db = out.add(given_or(on, a[9], [&] { return at::zeros({c.C}, f32); }));
         const at::Tensor ws = a[11] == Py_None ? bytes(u, ssd_conv_workspace_bytes(c.B, c.L, c.C)) : tensor(a[11]);
         const int rc = unlocked(ssd_conv_bwd, c.B, c.L, c.C, c.code, u.data_ptr(), c.bs, fptr(a[1]), fptr(a[2]), ptr(a[3]), ptr(a[4]), fptr(a[5]), ptr(du),
-                                    fptr(ds), fptr(dw), fptr(db), PyObject_IsTrue(a[10]), ws.data_ptr(), nbytes(ws), stream_of(a[12]));
+                                    fptr(ds), fptr(dw), fptr(db), PyObject_IsTrue(a[10]), ws.data_ptr(), nbytes(ws), on.st);
         if (rc) return PyLong_FromLong(rc);
         return out.tuple();
     });
@@ -269,9 +303,10 @@ PyObject *gated_norm_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded(n, 7, [&]() -> PyObject * {
         const at::Tensor &y = tensor(a[0]);
         const NormArgs c = norm_args(y, a[3]);
+        const CallStream on(a[6], y);
         Results out;
-        PyObject *o = out.add(given_or(a[5], [&] { return at::empty_like(y); }));
-        const int rc = unlocked(ssd_gated_norm_fwd, c.rows, c.D, c.group, c.code, y.data_ptr(), ptr(a[1]), fptr(a[2]), real(a[4]), ptr(o), stream_of(a[6]));
+        PyObject *o = out.add(given_or(on, a[5], [&] { return at::empty_like(y); }));
+        const int rc = unlocked(ssd_gated_norm_fwd, c.rows, c.D, c.group, c.code, y.data_ptr(), ptr(a[1]), fptr(a[2]), real(a[4]), ptr(o), on.st);
         if (rc) return PyLong_FromLong(rc);
         Py_INCREF(o);
         return o;
@@ -283,13 +318,14 @@ PyObject *gated_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded(n, 12, [&]() -> PyObject * {
         const at::Tensor &y = tensor(a[0]);
         const NormArgs c = norm_args(y, a[4]);
+        const CallStream on(a[11], y);
         Results out;
-        PyObject *dy = out.add(given_or(a[6], [&] { return at::empty_like(y); }));
-        PyObject *dz = out.add(given_or(a[7], [&] { return at::empty_like(y); }));
-        PyObject *dg = out.add(given_or(a[8], [&] { return at::zeros({c.D}, y.options().dtype(at::kFloat)); }));
+        PyObject *dy = out.add(given_or(on, a[6], [&] { return at::empty_like(y); }));
+        PyObject *dz = out.add(given_or(on, a[7], [&] { return at::empty_like(y); }));
+        PyObject *dg = out.add(given_or(on, a[8], [&] { return at::zeros({c.D}, y.options().dtype(at::kFloat)); }));
         const at::Tensor ws = a[10] == Py_None ? bytes(y, ssd_gated_norm_workspace_bytes(c.rows, c.D)) : tensor(a[10]);
         const int rc = unlocked(ssd_gated_norm_bwd, c.rows, c.D, c.group, c.code, y.data_ptr(), ptr(a[1]), fptr(a[2]), real(a[5]), ptr(a[3]), ptr(dy), ptr(dz),
-                                          fptr(dg), PyObject_IsTrue(a[9]), ws.data_ptr(), nbytes(ws), stream_of(a[11]));
+                                          fptr(dg), PyObject_IsTrue(a[9]), ws.data_ptr(), nbytes(ws), on.st);
         if (rc) return PyLong_FromLong(rc);
         return out.tuple();
     });
@@ -305,13 +341,13 @@ ssd_shape_t glue_shape(const at::Tensor &t) {
 PyObject *glue_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded(n, 5, [&]() -> PyObject * {
         const ssd_shape_t s = glue_shape(tensor(a[0]));
-        return PyLong_FromLong(unlocked(ssd_glue_fwd, &s, ptr(a[0]), ptr(a[1]), fptr(a[2]), ptr(a[3]), stream_of(a[4])));
+        return PyLong_FromLong(unlocked(ssd_glue_fwd, &s, ptr(a[0]), ptr(a[1]), fptr(a[2]), ptr(a[3]), CallStream(a[4], tensor(a[0])).st));
     });
 }
 PyObject *glue_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded(n, 4, [&]() -> PyObject * {
         const ssd_shape_t s = glue_shape(tensor(a[0]));
-        return PyLong_FromLong(unlocked(ssd_glue_bwd, &s, ptr(a[0]), fptr(a[1]), ptr(a[2]), stream_of(a[3])));
+        return PyLong_FromLong(unlocked(ssd_glue_bwd, &s, ptr(a[0]), fptr(a[1]), ptr(a[2]), CallStream(a[3], tensor(a[0])).st));
     });
 }
 
@@ -368,9 +404,9 @@ PyObject *packed_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded(n, 12, [&]() -> PyObject * {
         const at::Tensor &x = tensor(a[0]), &ph = tensor(a[7]), &pd = tensor(a[8]);
         require(x.is_cuda(), PyExc_ValueError, "device tensors required");
-        c10::cuda::CUDAGuard guard(x.device());
+        const CallStream on(a[11], x);
         Results out;
-        PyObject *y = out.add(given_or(a[9], [&] { return rows_like(x); }));
+        PyObject *y = out.add(given_or(on, a[9], [&] { return rows_like(x); }));
         const ssd_rows_t s = rows_shape(a, tensor(y));
         on_device(pd, x.device());
         const size_t need = a[10] == Py_None ? ssd_packed_workspace_bytes(&s, ph.data_ptr()) : 1;
@@ -378,8 +414,9 @@ PyObject *packed_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const at::Tensor ws = a[10] == Py_None ? bytes(x, need) : tensor(a[10]);
         on_device(ws, x.device());
         const int rc = unlocked(ssd_packed_fwd, &s, ph.data_ptr(), pd.data_ptr(), x.data_ptr(), fptr(a[1]), fptr(a[2]), ptr(a[3]), ptr(a[4]), fptr(a[5]), fptr(a[6]),
-                                ptr(y), ws.data_ptr(), nbytes(ws), stream_of(a[11]));
+                                ptr(y), ws.data_ptr(), nbytes(ws), on.st);
         if (rc) return PyLong_FromLong(rc);
+        on.uses(pd);
         Py_INCREF(y);
         return y;
     });
@@ -390,13 +427,13 @@ PyObject *decode_slots(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded(n, 10, [&]() -> PyObject * {
         const at::Tensor &x = tensor(a[0]);
         require(x.is_cuda(), PyExc_ValueError, "device tensors required");
-        c10::cuda::CUDAGuard guard(x.device());
+        const CallStream on(a[9], x);
         Results out;
-        PyObject *y = out.add(given_or(a[8], [&] { return rows_like(x); }));
+        PyObject *y = out.add(given_or(on, a[8], [&] { return rows_like(x); }));
         const ssd_rows_t s = rows_shape(a, tensor(y));
         const int32_t *slots = slots_of(a[7], s.rows, x.device());
         const int rc = unlocked(ssd_decode_slots, &s, x.data_ptr(), fptr(a[1]), fptr(a[2]), ptr(a[3]), ptr(a[4]), fptr(a[5]), fptr(a[6]), slots, ptr(y),
-                                stream_of(a[9]));
+                                on.st);
         if (rc) return PyLong_FromLong(rc);
         Py_INCREF(y);
         return y;
@@ -427,14 +464,15 @@ PyObject *conv_packed_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded(n, 8, [&]() -> PyObject * {
         const at::Tensor &u = tensor(a[0]), &ph = tensor(a[4]), &pd = tensor(a[5]);
         require(u.is_cuda(), PyExc_ValueError, "device tensors required");
-        c10::cuda::CUDAGuard guard(u.device());
+        const CallStream on(a[7], u);
         Results out;
-        PyObject *o = out.add(given_or(a[6], [&] { return rows_like(u); }));
+        PyObject *o = out.add(given_or(on, a[6], [&] { return rows_like(u); }));
         const ConvRows c = conv_rows(a, tensor(o));
         on_device(pd, u.device());
         const int rc = unlocked(ssd_conv_packed_fwd, ph.data_ptr(), pd.data_ptr(), c.rows, c.C, c.code, u.data_ptr(), c.u_rs, fptr(a[1]), fptr(a[2]), ptr(a[3]),
-                                c.nslots, c.state_rs, ptr(o), c.out_rs, stream_of(a[7]));
+                                c.nslots, c.state_rs, ptr(o), c.out_rs, on.st);
         if (rc) return PyLong_FromLong(rc);
+        on.uses(pd);
         Py_INCREF(o);
         return o;
     });
@@ -445,13 +483,13 @@ PyObject *conv_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded(n, 7, [&]() -> PyObject * {
         const at::Tensor &u = tensor(a[0]);
         require(u.is_cuda(), PyExc_ValueError, "device tensors required");
-        c10::cuda::CUDAGuard guard(u.device());
+        const CallStream on(a[6], u);
         Results out;
-        PyObject *o = out.add(given_or(a[5], [&] { return rows_like(u); }));
+        PyObject *o = out.add(given_or(on, a[5], [&] { return rows_like(u); }));
         const ConvRows c = conv_rows(a, tensor(o));
         const int32_t *slots = slots_of(a[4], c.rows, u.device());
         const int rc = unlocked(ssd_conv_step, c.rows, c.C, c.code, u.data_ptr(), c.u_rs, fptr(a[1]), fptr(a[2]), ptr(a[3]), c.nslots, c.state_rs, slots, ptr(o),
-                                c.out_rs, stream_of(a[6]));
+                                c.out_rs, on.st);
         if (rc) return PyLong_FromLong(rc);
         Py_INCREF(o);
         return o;
@@ -466,7 +504,7 @@ PyObject *grad_clip(PyObject *, PyObject *const *a, Py_ssize_t n) {
         require(k > 0 && (a[2] == Py_None || PyList_GET_SIZE(a[2]) == k), PyExc_ValueError, "one output for each gradient is required, and one gradient at least");
         const at::Device dev = tensor(PyList_GET_ITEM(a[0], 0)).device();
         require(dev.is_cuda(), PyExc_ValueError, "device tensors required");
-        c10::cuda::CUDAGuard guard(dev);
+        const CallStream on(a[4], tensor(PyList_GET_ITEM(a[0], 0)));
         std::vector<const void *> in(k);
         std::vector<void *> to(k);
         std::vector<int64_t> numel(k);
@@ -486,9 +524,9 @@ PyObject *grad_clip(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const at::Tensor ws = a[3] == Py_None ? bytes(first, ssd_grad_clip_workspace_bytes((int)k)) : tensor(a[3]);
         on_device(ws, dev);
         Results out;
-        PyObject *norm = out.add(THPVariable_Wrap(f32_like(first, {})));
+        PyObject *norm = out.add(THPVariable_Wrap(on.result(f32_like(first, {}))));
         const int rc = unlocked(ssd_grad_clip, (int)k, in.data(), to.data(), numel.data(), code.data(), real(a[1]), fptr(norm), ws.data_ptr(), nbytes(ws),
-                                stream_of(a[4]));
+                                on.st);
         if (rc) return PyLong_FromLong(rc);
         Py_INCREF(norm);
         return norm;

@@ -1,6 +1,8 @@
 """Python binding of libssd (include/ssd.h).  Argument marshalling only: every step of the path
 runs in the library's CUDA kernels.  The calls that launch work go through the native module built from
 csrc/binding.cpp, queries and the rest through ctypes.  torch is used for device memory and streams, nothing else.
+What a call allocates itself (results and scratch that it is not given) belongs to the stream that it launches on; the memory of its arguments is the
+caller's, who keeps it until the work is done.  A status (poll_status) can be read of a scratch that the caller gives.
 There is no CPU fallback: if the shared library has not been built, loading raises.
 """
 import ctypes
@@ -234,6 +236,19 @@ def _check_inputs(x, dt, A, Bm, Cm, D):
         raise TypeError("Bm, Cm must have the dtype of x")
 
 
+def _of_stream(stream, make):
+    """A dict of new tensors in memory of a call's stream (as CallStream in csrc/binding.cpp has it)."""
+    now = torch.cuda.current_stream()
+    if stream is None or stream.cuda_stream == now.cuda_stream:
+        return make()
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream.cuda_stream) if stream.cuda_stream else torch.cuda.default_stream()):
+        out = make()
+    for t in out.values():
+        if t is not None:
+            t.record_stream(now)
+    return out
+
+
 def ssd_fwd(x, dt, A, Bm, Cm, D, h0=None, *, chunk, seg=0, flags=0, y=None, h_final=None,
             ws=None, stream=None):
     """y, h_final = SSD forward (Eq. 1).  `seg` only sizes the scratch."""
@@ -274,11 +289,10 @@ def ssd_bwd_segmented(x, dt, A, Bm, Cm, D, boundary, dy, dh_final=None, *, chunk
     if out is None:
         B, _, H, P = x.shape
         N, dev = Bm.shape[3], x.device
-        out = dict(dx=torch.empty_like(x), ddt=torch.empty_like(dt),
-                   dA=torch.empty(H, dtype=torch.float32, device=dev),
-                   dB=torch.empty_like(Bm), dC=torch.empty_like(Cm),
-                   dD=torch.empty(H, dtype=torch.float32, device=dev),
-                   dh0=torch.empty(B, H, P, N, dtype=torch.float32, device=dev) if want_dh0 else None)
+        out = _of_stream(stream, lambda: dict(
+            dx=torch.empty_like(x), ddt=torch.empty_like(dt), dA=torch.empty(H, dtype=torch.float32, device=dev),
+            dB=torch.empty_like(Bm), dC=torch.empty_like(Cm), dD=torch.empty(H, dtype=torch.float32, device=dev),
+            dh0=torch.empty(B, H, P, N, dtype=torch.float32, device=dev) if want_dh0 else None))
     rc = (_nat or _native()).bwd(x, dt, A, Bm, Cm, D, boundary, dy, dh_final, chunk, seg, flags, out["dx"], out["ddt"], out["dA"],
                                  out["dB"], out["dC"], out["dD"], out.get("dh0"), ws, stream)
     if rc != SSD_OK:
@@ -371,7 +385,7 @@ class PackedPlan:
     """Plan of a batch of packed prompts (include/ssd.h): sequence i has rows cu_seqlens[i] to cu_seqlens[i+1] - 1 of the tensors, its state
     in slot slots[i] of the cache (-1: kept nowhere; None: slot i), and goes on from that state where carry[i] is true (None: all start from
     zeros).  Made once per batch, for layers of `heads` heads, and used by every call on it; the copy on the device is complete when the
-    constructor returns."""
+    constructor returns, and is kept until the calls on it are done."""
 
     def __init__(self, cu_seqlens, *, slots=None, carry=None, nslots=None, heads, device="cuda"):
         cu = torch.as_tensor(cu_seqlens, dtype=torch.int64, device="cpu").contiguous()
@@ -412,7 +426,8 @@ def alloc_packed_workspace(plan, x, Bm):
 
 def ssd_packed_fwd(plan, x, dt, A, Bm, Cm, D, state, *, y=None, ws=None, stream=None):
     """y [rows, H, P] of Eq. 1 over the plan's sequences; state [nslots, H, P, N] fp32 is advanced in place.  x, Bm [rows, G, N], Cm and dt
-    [rows, H] may have row strides (columns of a wider tensor).  Rows of y behind the last sequence are left as they are."""
+    [rows, H] may have row strides (columns of a wider tensor).  Rows of y behind the last sequence are left as they are.  A ws of the caller's
+    (alloc_packed_workspace) has the status that poll_status reads."""
     r = (_nat or _native()).packed_fwd(x, dt, A, Bm, Cm, D, state, plan.host, plan.dev, y, ws, stream)
     if r.__class__ is int:
         raise SSDError(r, "ssd_packed_fwd")
