@@ -1,7 +1,7 @@
 // The short causal convolution over packed prompts: sequences one behind the other in the rows of u and out, the three inputs in front of
 // each and the last three of it in a slot of a cache.
 //     out[t,c] = SiLU(bias[c] + sum_{k<4} w[c,k] u[t-3+k, c])
-// A CTA takes a tile of rows of one sequence (32; fewer in small batches, PlanHeader's maker decides); a thread has 16 bytes of adjacent channels
+// A CTA takes a tile of rows of one sequence (64; 32, 16 or 8 in batches of up to 16384, 4096, 1024 rows: ssd_plan_make); a thread has 16 bytes of adjacent channels
 // and walks the rows with the last three in registers.  Its 16 bytes of the next 16 rows are on their way into shared memory, where no other
 // thread looks (so there is nothing to meet for): 23760 rows of 5376 channels in bf16 98 us (5.2 TB/s, 80% of a copy's rate), with loads to registers
 // ahead of their use 128.  Bound by memory.  The tile with a sequence's first row is the only one that touches its slot:
