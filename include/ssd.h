@@ -268,8 +268,8 @@ int ssd_gated_norm_bwd(long long rows, int D, int group, int dtype, const void *
  * (The paper runs one sequence; these are Eq. 1 and the convolution for batches as a server has them.)
  *
  * A batch of prompts is packed: the rows of sequence i are rows cu_seqlens[i] to cu_seqlens[i+1] - 1 of the tensors, any number of them,
- * none included.  Rows behind the last sequence are not written, and what they hold has no effect.  Its plan is made on the host, once for all
- * layers:
+ * none included.  Rows behind the last sequence are not written, and what they hold has no effect.  A batch whose sequences are all empty may
+ * have tensors of no rows (pointers to them may be NULL then): its calls set slots to zeros.  The plan is made on the host, once for all layers:
  *   cu_seqlens  HOST [nseq + 1], not decreasing, the first 0
  *   slots       HOST [nseq] or NULL (slot i): where sequence i's state is kept, below nslots; -1: nowhere, it starts from zeros and its last
  *               state is dropped.  No slot twice.
@@ -290,7 +290,7 @@ int ssd_plan_make(int nseq, const int64_t *cu_seqlens, const int32_t *slots, con
  * bytes, so that x, Bm, Cm may be columns of one wider tensor.  dt needs no alignment beyond its type's.
  */
 typedef struct ssd_rows {
-    int64_t rows;                  /* of x, y, dt, Bm, Cm */
+    int64_t rows;                  /* of x, y, dt, Bm, Cm; for ssd_decode_slots one at least */
     int32_t H, P, N, G;            /* P = 64, N in {64, 128} */
     int32_t dtype;                 /* SSD_DTYPE_* : type of x, Bm, Cm, y */
     int32_t nslots;
@@ -326,7 +326,7 @@ int ssd_decode_slots(const ssd_rows_t *shape, const void *x, const float *dt, co
 
 /*
  * The convolution of ssd_conv_fwd over packed prompts (rows of u and out as in a plan's sequences, C % 8 == 0, row strides in elements, 0 =
- * dense, multiples of 16 bytes) and for one token of each running sequence (slots as for ssd_decode_slots; rows <= 65535).
+ * dense, multiples of 16 bytes) and for one token of each running sequence (slots as for ssd_decode_slots; 1 <= rows <= 65535).
  *   state [nslots, 3, C] I/O dtype, state_stride elements between slots (0 = 3 C; a multiple of 16 bytes): the last three inputs of a
  *         sequence, which the step moves on by one; sequences of fewer rows keep the rest of the old ones (carry) or zeros
  * out and u have no element in common (else SSD_EINVAL).  Return values as above.

@@ -1063,9 +1063,9 @@ int ssd_plan_make(int nseq, const int64_t *cu_seqlens, const int32_t *slots, con
     return SSD_OK;
 }
 
-// Row and slot strides of a cache call
-static int rows_check(const ssd_rows_t *s, ssd_rows_t &r) {
-    if (!s || s->rows <= 0 || s->rows > INT32_MAX || s->H <= 0 || s->G <= 0 || s->H % s->G || s->nslots <= 0) return SSD_EINVAL;
+// Row and slot strides of a cache call.  `least`: 0 where a batch of empty sequences has no rows at all
+static int rows_check(const ssd_rows_t *s, ssd_rows_t &r, int least) {
+    if (!s || s->rows < least || s->rows > INT32_MAX || s->H <= 0 || s->G <= 0 || s->H % s->G || s->nslots <= 0) return SSD_EINVAL;
     if (s->P != 64 || (s->N != 64 && s->N != 128) || s->H > 65535) return SSD_EUNSUPPORTED;
     if (s->dtype != SSD_DTYPE_F32 && s->dtype != SSD_DTYPE_BF16) return SSD_EUNSUPPORTED;
     r = *s;
@@ -1083,6 +1083,7 @@ static int rows_check(const ssd_rows_t *s, ssd_rows_t &r) {
 
 // Whether an output's rows and an input's have an element in common; both may be columns of one wider tensor
 static bool rows_meet(const void *out, int64_t out_rs, int64_t out_cols, const void *in, int64_t in_rs, int64_t in_cols, int64_t rows, int64_t e) {
+    if (rows == 0) return false;
     const int64_t a = (int64_t)(uintptr_t)out, b = (int64_t)(uintptr_t)in;
     if (a >= b + ((rows - 1) * in_rs + in_cols) * e || b >= a + ((rows - 1) * out_rs + out_cols) * e) return false;
     if (out_rs != in_rs) return true;
@@ -1100,17 +1101,18 @@ static bool plan_fits(const PlanHeader *h, int64_t rows, int nslots) { return h 
 size_t ssd_packed_workspace_bytes(const ssd_rows_t *shape, const void *plan_host) {
     ssd_rows_t r;
     const PlanHeader *h = (const PlanHeader *)plan_host;
-    if (rows_check(shape, r) || !plan_fits(h, r.rows, r.nslots)) return 0;
+    if (rows_check(shape, r, 0) || !plan_fits(h, r.rows, r.nslots)) return 0;
     return 256 + (size_t)h->entries * r.H * (64 * r.N * sizeof(float) + sizeof(double)) + 16;
 }
 
 int ssd_packed_fwd(const ssd_rows_t *shape, const void *plan_host, const void *plan_dev, const void *x, const float *dt, const float *A, const void *Bm,
                    const void *Cm, const float *D, float *state, void *y, void *ws, size_t ws_bytes, void *stream) {
     ssd_rows_t r;
-    int rc = rows_check(shape, r);
+    int rc = rows_check(shape, r, 0);
     if (rc) return rc;
     const PlanHeader *h = (const PlanHeader *)plan_host;
-    if (!plan_dev || !x || !dt || !A || !Bm || !Cm || !D || !state || !y || !ws || !plan_fits(h, r.rows, r.nslots) || h->heads != r.H) return SSD_EINVAL;
+    if (r.rows && (!x || !dt || !Bm || !Cm || !y)) return SSD_EINVAL;
+    if (!plan_dev || !A || !D || !state || !ws || !plan_fits(h, r.rows, r.nslots) || h->heads != r.H) return SSD_EINVAL;
     if (misaligned(plan_dev) || misaligned(x) || ((uintptr_t)dt & 3) || ((uintptr_t)A & 3) || misaligned(Bm) || misaligned(Cm) || ((uintptr_t)D & 3) ||
         misaligned(state) || misaligned(y))
         return SSD_EALIGN;
@@ -1122,7 +1124,7 @@ int ssd_packed_fwd(const ssd_rows_t *shape, const void *plan_host, const void *p
     PackedParams p = {};
     p.H = r.H, p.G = r.G, p.N = r.N, p.dtype = r.dtype, p.hpg = hpg;
     p.nunits = h->nunits, p.nsums = h->nsums;
-    p.tc = r.dtype == SSD_DTYPE_BF16;
+    p.tc = r.dtype == SSD_DTYPE_BF16 && r.rows;         // without rows there is nothing to make tensor maps of, and no type to read
     p.per_cta = hpg > 1 && heads_by_twos(h->nunits, r.H) ? 2 : 1;
     p.head_sets = r.G * ((hpg + p.per_cta - 1) / p.per_cta);
     if ((long long)h->nunits * p.head_sets > INT32_MAX) return SSD_EUNSUPPORTED;
@@ -1143,7 +1145,7 @@ int ssd_packed_fwd(const ssd_rows_t *shape, const void *plan_host, const void *p
 int ssd_decode_slots(const ssd_rows_t *shape, const void *x, const float *dt, const float *A, const void *Bm, const void *Cm, const float *D, float *state,
                      const int32_t *slots, void *y, void *stream) {
     ssd_rows_t r;
-    int rc = rows_check(shape, r);
+    int rc = rows_check(shape, r, 1);
     if (rc) return rc;
     if (!x || !dt || !A || !Bm || !Cm || !D || !state || !y || (!slots && r.rows > r.nslots)) return SSD_EINVAL;
     if (r.rows > 65535 || r.rows * r.H * 2 > INT32_MAX) return SSD_EUNSUPPORTED;        // a row looks at all slots in front of its own
@@ -1161,8 +1163,8 @@ int ssd_decode_slots(const ssd_rows_t *shape, const void *x, const float *dt, co
 }
 
 // Convolution with a cache: rows of u and out, slots of the cache
-static int conv_rows_check(long long rows, int C, int dtype, int nslots, long long &u_rs, long long &out_rs, long long &state_stride) {
-    if (rows <= 0 || rows > INT32_MAX || C <= 0 || C % 8 || nslots <= 0) return SSD_EINVAL;
+static int conv_rows_check(long long rows, int least, int C, int dtype, int nslots, long long &u_rs, long long &out_rs, long long &state_stride) {
+    if (rows < least || rows > INT32_MAX || C <= 0 || C % 8 || nslots <= 0) return SSD_EINVAL;
     if (dtype != SSD_DTYPE_F32 && dtype != SSD_DTYPE_BF16) return SSD_EUNSUPPORTED;
     if (C > (1 << 23)) return SSD_EUNSUPPORTED;
     if (!u_rs) u_rs = C;
@@ -1176,10 +1178,10 @@ static int conv_rows_check(long long rows, int C, int dtype, int nslots, long lo
 
 int ssd_conv_packed_fwd(const void *plan_host, const void *plan_dev, long long rows, int C, int dtype, const void *u, long long u_rstride, const float *w,
                         const float *bias, void *state, int nslots, long long state_stride, void *out, long long out_rstride, void *stream) {
-    int rc = conv_rows_check(rows, C, dtype, nslots, u_rstride, out_rstride, state_stride);
+    int rc = conv_rows_check(rows, 0, C, dtype, nslots, u_rstride, out_rstride, state_stride);
     if (rc) return rc;
     const PlanHeader *h = (const PlanHeader *)plan_host;
-    if (!plan_dev || !u || !w || !bias || !state || !out || !plan_fits(h, rows, nslots)) return SSD_EINVAL;
+    if ((rows && (!u || !out)) || !plan_dev || !w || !bias || !state || !plan_fits(h, rows, nslots)) return SSD_EINVAL;
     if (misaligned(plan_dev) || misaligned(u) || misaligned(w) || misaligned(bias) || misaligned(state) || misaligned(out)) return SSD_EALIGN;
     if (rows_meet(out, out_rstride, C, u, u_rstride, C, rows, dtype == SSD_DTYPE_BF16 ? 2 : 4)) return SSD_EINVAL;
     rc = check_device();
@@ -1192,7 +1194,7 @@ int ssd_conv_packed_fwd(const void *plan_host, const void *plan_dev, long long r
 
 int ssd_conv_step(long long rows, int C, int dtype, const void *u, long long u_rstride, const float *w, const float *bias, void *state, int nslots,
                   long long state_stride, const int32_t *slots, void *out, long long out_rstride, void *stream) {
-    int rc = conv_rows_check(rows, C, dtype, nslots, u_rstride, out_rstride, state_stride);
+    int rc = conv_rows_check(rows, 1, C, dtype, nslots, u_rstride, out_rstride, state_stride);
     if (rc) return rc;
     if (!u || !w || !bias || !state || !out || (!slots && rows > nslots)) return SSD_EINVAL;
     if (rows > 65535) return SSD_EUNSUPPORTED;
