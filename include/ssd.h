@@ -342,8 +342,9 @@ int ssd_conv_step(long long rows, int C, int dtype, const void *u, long long u_r
  *   grads, outs, numel, dtypes  HOST arrays [n] (read before return) of device pointers, element counts (0 allowed) and SSD_DTYPE_*; an
  *          output has its gradient's type and is the gradient itself or a buffer of its own; no output meets another, or another's
  *          gradient.  Addresses need the alignment of the type only.
- *   norm   DEVICE fp32 or NULL: the norm before clipping.  Sums are kept in 64 bits: no value of fp32 overflows or vanishes in them.  A norm
- *          that is not finite scales nothing (factor 1): look at it before the step.
+ *   norm   DEVICE fp32 or NULL: the norm before clipping.  Up to 16 squares are added in fp32 (in 64 bits where they leave the middle of its range),
+ *          everything above in 64 bits: no value of fp32 overflows or vanishes in them.  With a gradient that is not finite nothing is scaled
+ *          (factor 1): look at the norm before the step.  A finite norm above fp32's largest value is given as infinity, and scales.
  *   ws     ssd_grad_clip_workspace_bytes(n) bytes, 256-byte aligned
  * Deterministic.  Returns SSD_OK or SSD_EINVAL / SSD_EUNSUPPORTED / SSD_EALIGN / SSD_EWORKSPACE / SSD_EDEVICE / SSD_ECUDA.
  */

@@ -1,5 +1,7 @@
 // The norm of many gradients together and their scaling to a largest norm:
-//     norm = sqrt(sum g^2) ,   out = g min(1, max_norm / norm)          (a norm that is not finite scales nothing)
+//     norm = sqrt(sum g^2) ,   out = g min(1, max_norm / norm)          (gradients that are not finite: nothing is scaled)
+// The factor is fp32.  A norm above fp32's largest value, or a factor below its smallest normal one, which would have few bits left, are kept in 64
+// bits, and the gradients then multiplied so, one by one.
 // Two launches.  The first walks all tensors in chunks, a number of CTAs that the sizes fix, and leaves one sum per CTA in 64 bits;
 // in the second every CTA adds those sums up in the same order and scales its chunks, the last read first, which the L2 cache still
 // holds.  Squares of up to 16 elements are added in 32 bits, everything above in 64; those whose sum leaves the middle of the range (below
@@ -7,6 +9,8 @@
 // Bound by memory: 483 MB of gradients 241 us, two readings and a writing at 6.0 TB/s (75 us the norm, at 6.4).  384 small vectors take 18 us
 // on the device, 24 with the host's part of the call, which is the longer one.
 // The table of tensors travels in the launch's parameters: no copy to the device, and a captured graph has it by value.
+#include <cfloat>
+
 #include "ssd_internal.h"
 
 namespace ssd {
@@ -169,6 +173,18 @@ template <int MAX> __global__ void __launch_bounds__(CL_THREADS) k_clip_norm(con
     if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
+// All chunks by a factor below fp32's normal numbers
+template <int MAX> __device__ __noinline__ void scale_64(const ClipTable<MAX> &tab, double scale) {
+    for (int c = blockIdx.x; c < tab.chunks; c += gridDim.x) {
+        const ClipTensor &t = tab.t[find_tensor(tab, c)];
+        const int64_t per = chunk_elems(t.dtype), begin = (c - t.first) * per, end = min(begin + per, t.n);
+        for (int64_t at = begin + threadIdx.x; at < end; at += CL_THREADS) {
+            if (t.dtype == SSD_DTYPE_F32) ((float *)t.out)[at] = (float)((double)((const float *)t.in)[at] * scale);
+            else ((__nv_bfloat16 *)t.out)[at] = __float2bfloat16_rn((float)((double)__bfloat162float(((const __nv_bfloat16 *)t.in)[at]) * scale));
+        }
+    }
+}
+
 template <int MAX>
 __global__ void __launch_bounds__(CL_THREADS, CL_SCALE) k_clip_scale(const __grid_constant__ ClipTable<MAX> tab, const double *part, int nparts, float max_norm, float *norm) {
     __shared__ double red[CL_THREADS / 32];
@@ -176,9 +192,14 @@ __global__ void __launch_bounds__(CL_THREADS, CL_SCALE) k_clip_scale(const __gri
     pdl_wait();
     double s = 0.;
     for (int i = threadIdx.x; i < nparts; i += CL_THREADS) s += part[i];
-    const float n = (float)sqrt(block_sum(s, red));
+    const double wide = sqrt(block_sum(s, red));
+    const float n = (float)wide;
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = n;
-    const float scale = n > max_norm && isfinite(n) ? max_norm / n : 1.f;
+    const float scale = n > max_norm && isfinite(wide) ? max_norm / n : 1.f;
+    if (scale < FLT_MIN && max_norm > 0.f) {
+        scale_64(tab, max_norm / wide);
+        return;
+    }
     for (int c = tab.chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
         const ClipTensor &t = tab.t[find_tensor(tab, c)];
         if (scale == 1.f && t.in == t.out) continue;

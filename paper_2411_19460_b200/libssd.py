@@ -471,7 +471,7 @@ def alloc_grad_clip_workspace(grads):
 
 def ssd_grad_clip(grads, max_norm, *, out=None, ws=None, stream=None):
     """Norm of all gradients together (fp32, on the device); the gradients are scaled by min(1, max_norm / norm), in place or into the tensors
-    of `out`.  A norm that is not finite scales nothing."""
+    of `out`.  Where a gradient is not finite nothing is scaled; a finite norm above fp32's largest value is given as infinity, and scales."""
     r = (_nat or _native()).grad_clip(list(grads), max_norm, None if out is None else list(out), ws, stream)
     if r.__class__ is int:
         raise SSDError(r, "ssd_grad_clip")
