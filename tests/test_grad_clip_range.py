@@ -50,3 +50,18 @@ def test_a_norm_above_fp32_and_no_limit():
     grads = [torch.full((1000,), 3e38, device="cuda")]
     assert float(libssd.ssd_grad_clip(grads, math.inf)) == math.inf and bool((grads[0] == 3e38).all())
     assert float(libssd.ssd_grad_clip(grads, 0.0)) == math.inf and bool((grads[0] == 0).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_zeros_among_the_gradients(dtype):
+    """Zeros of either sign, whole vectors and chunks of them, and next to squares that leave fp32: the same norm as without them."""
+    g = torch.Generator().manual_seed(2)
+    for scale in (1.0, 1e-25):
+        v = (torch.randn(40000, generator=g) * scale).to(dtype)
+        v[:9000] = 0
+        v[20000:20016] = -0.0
+        v[20024:20031] = 0
+        v[30000:30007] = 0
+        got = float(libssd.ssd_grad_clip([v.cuda(), torch.zeros(50000, dtype=dtype, device="cuda")], math.inf))
+        assert abs(got - norm_of([v])) <= 2.0 ** -21 * norm_of([v])
