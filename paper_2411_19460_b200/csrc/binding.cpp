@@ -514,7 +514,7 @@ PyObject *grad_clip(PyObject *, PyObject *const *a, Py_ssize_t n) {
             on_device(g, dev);
             on_device(o, dev);
             code[i] = dtype_code(g, "gradients must be float32 or bfloat16");
-            require(o.scalar_type() == g.scalar_type() && o.numel() == g.numel(), PyExc_ValueError, "an output must have its gradient's type and size");
+            require(o.scalar_type() == g.scalar_type() && o.sizes() == g.sizes(), PyExc_ValueError, "an output must have its gradient's type and shape");
             require(g.is_contiguous() && o.is_contiguous(), PyExc_ValueError, "gradients and outputs must be contiguous");
             in[i] = g.data_ptr();
             to[i] = o.data_ptr();

@@ -65,3 +65,11 @@ def test_zeros_among_the_gradients(dtype):
         v[30000:30007] = 0
         got = float(libssd.ssd_grad_clip([v.cuda(), torch.zeros(50000, dtype=dtype, device="cuda")], math.inf))
         assert abs(got - norm_of([v])) <= 2.0 ** -21 * norm_of([v])
+
+
+@pytest.mark.gpu
+def test_an_output_has_its_gradients_shape():
+    g = torch.randn(6, 8, device="cuda")
+    for shape in ((48,), (8, 6), (1, 6, 8)):
+        with pytest.raises(ValueError):
+            libssd.ssd_grad_clip([g], 1.0, out=[torch.empty(shape, device="cuda")])
