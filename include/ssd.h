@@ -308,8 +308,9 @@ typedef struct ssd_rows {
  * state in front of 128 rows are operands of two bf16 parts, 2^-16 of each of their terms; D x is added in fp32, and the result rounded once.
  * A plan may cut a long sequence into ranges of whole 128 rows, whose states are then joined from sums: the bits of a result depend on the
  * plan, not on other calls or on what ws holds, and repeat.  A value that is not finite stays in its sequence, in its row's block of 128
- * rows and what follows.  Calls that share ws, on one stream or in graphs, run one after the other; ws is used from the first launch to
- * the last, its first word is the status that ssd_poll_status reads.
+ * rows and what follows; infinities come out as infinities where the formulas have them with fp32 tensors, as infinities or NaN with bf16
+ * ones.  Calls that share ws, on one stream or in graphs, run one after the other; ws is used from the first launch to the last, its first
+ * word is the status that ssd_poll_status reads.
  * Returns SSD_OK or SSD_EINVAL / SSD_EUNSUPPORTED / SSD_EALIGN / SSD_EWORKSPACE / SSD_EDEVICE / SSD_ECUDA.
  */
 size_t ssd_packed_workspace_bytes(const ssd_rows_t *shape, const void *plan_host);

@@ -6,7 +6,7 @@
 //     h_out = e^{cs_last} h_in + sum_s e^{cs_last-cs_s} dt_s x_s B_s^T
 // A CTA takes one head of one sequence from its first row to its last, the state in registers (fp32) all the way: nothing but the
 // tensors of the call is moved.  The products are those of the split path (ssd_split.cuh): fp32 operands as three bf16 parts, so that
-// states and outputs are fp32 results: fp32 tensors (bf16 ones: ssd_packed_tc.cu).  A last chunk that the sequence does not fill is
+// states and outputs are fp32 results, infinities among them: fp32 tensors (bf16 ones: ssd_packed_tc.cu).  A last chunk that the sequence does not fill is
 // filled with zeros, whatever the rows behind it hold.  cs in 64 bits: with strong decays it runs into the thousands, where 32 bits
 // would leave 5e-4 of a difference.
 //
@@ -51,18 +51,22 @@ __device__ __forceinline__ void put_acc(SplitTile *s, const Acc &a) {
         }
 }
 
-template <int N, bool SUMS>
-__global__ void __launch_bounds__(PK_THREADS, N == 64 ? 2 : 1) k_packed_split(PackedParams p) {
+struct ChunkVecs {
+    double cs[PK_Q];
+    float dts[PK_Q], wS[PK_Q], eC[PK_Q];
+};
+
+// A CTA's work.  True where NaN came out without AGAIN: then it is run once more with it, for infinities (tile_mma), and writes its outputs a second time;
+// the slot is replaced at the end, by whichever is the last.
+template <int N, bool SUMS, bool AGAIN> __device__ __forceinline__ bool packed_unit(const PackedParams &p, ChunkVecs &vecs) {
     constexpr int NT = N / 64;
     extern __shared__ __align__(16) unsigned char pk_smem[];
     SplitTile *Cs = reinterpret_cast<SplitTile *>(pk_smem), *Bs = Cs + NT * PA, *Xs = Bs + NT * PA, *Hs = Xs + PA, *Ms = Hs;
-    __shared__ double cs[PK_Q];
-    __shared__ float dts[PK_Q], wS[PK_Q], eC[PK_Q];
-
-    pdl_launch_dependents();
-    pdl_wait();
-    // no wait of this kernel can run out: the status word is cleared, by the call's first launch
-    if ((SUMS || p.nsums == 0) && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = 0u;
+    double *cs = vecs.cs;
+    float *dts = vecs.dts, *wS = vecs.wS, *eC = vecs.eC;
+    bool nan = false;
+    // v times a decay, and c added.  A decay is above zero, so that an infinity stays one where the decay's fp32 value has become zero.
+    auto decayed_plus = [](float v, float decay, float c) { return AGAIN && isinf(v) ? v + c : fmaf(v, decay, c); };
     const int h = blockIdx.y, g = h / p.hpg;
     const ScanUnit u = (SUMS ? p.sums : p.units)[blockIdx.x];
     const float Dh = __ldg(p.D + h);
@@ -98,7 +102,7 @@ __global__ void __launch_bounds__(PK_THREADS, N == 64 ? 2 : 1) k_packed_split(Pa
             const float d = exp2f((float)p.decays[(int64_t)(u.entry + k) * p.H + h]);
             each([&](int i, int j, int half, int at) {
                 const float2 v = *reinterpret_cast<const float2 *>(entry + k * HPN + at), o = hs[i].get(j, half);
-                hs[i].set(j, half, make_float2(fmaf(o.x, d, v.x), fmaf(o.y, d, v.y)));
+                hs[i].set(j, half, make_float2(decayed_plus(o.x, d, v.x), decayed_plus(o.y, d, v.y)));
             });
         }
     }
@@ -148,21 +152,22 @@ __global__ void __launch_bounds__(PK_THREADS, N == 64 ? 2 : 1) k_packed_split(Pa
             yi.zero();
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
-                tile_mma<PA, PA, false, false, false>(m, Cs + i * PA, Bs + i * PA);
-                tile_mma<PA, 3, false, false, false>(yi, Cs + i * PA, Hs + 3 * i);
+                tile_mma<PA, PA, false, false, AGAIN>(m, Cs + i * PA, Bs + i * PA);
+                tile_mma<PA, 3, false, false, AGAIN>(yi, Cs + i * PA, Hs + 3 * i);
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int t = acc_row(i >> 1), s = acc_col(j) + (i & 1);
-                    m.m[j][i] = s <= t ? m.m[j][i] * (expf((float)(cs[t] - cs[s])) * dts[s]) : 0.f;
+                    if (AGAIN && s <= t && isinf(m.m[j][i])) m.m[j][i] *= dts[s];
+                    else m.m[j][i] = s <= t ? m.m[j][i] * (expf((float)(cs[t] - cs[s])) * dts[s]) : 0.f;
                 }
             __syncthreads();                                  // every warp is through with the state's parts
             put_acc(Ms, m);
             __syncthreads();
             yx.zero();
-            tile_mma<3, PA, false, true, false>(yx, Ms, Xs);
+            tile_mma<3, PA, false, true, AGAIN>(yx, Ms, Xs);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int t = acc_row(half);
@@ -171,8 +176,11 @@ __global__ void __launch_bounds__(PK_THREADS, N == 64 ? 2 : 1) k_packed_split(Pa
                 for (int j = 0; j < 4; ++j) {
                     const float2 a = yi.get(j, half), b = yx.get(j, half);
                     const float x0 = joined<PA>(Xs, t, acc_col(j)), x1 = joined<PA>(Xs, t, acc_col(j) + 1);
-                    const float2 v = make_float2(fmaf(Dh, x0, fmaf(e, a.x, b.x)), fmaf(Dh, x1, fmaf(e, a.y, b.y)));
-                    if (t < n) *reinterpret_cast<float2 *>(y + (t0 + t) * p.y_rs + acc_col(j)) = v;
+                    const float2 v = make_float2(fmaf(Dh, x0, decayed_plus(a.x, e, b.x)), fmaf(Dh, x1, decayed_plus(a.y, e, b.y)));
+                    if (t < n) {
+                        *reinterpret_cast<float2 *>(y + (t0 + t) * p.y_rs + acc_col(j)) = v;
+                        if (!AGAIN) nan |= isnan(v.x) || isnan(v.y);
+                    }
                 }
             }
             __syncthreads();                                  // every warp is through with the masked tile
@@ -181,9 +189,9 @@ __global__ void __launch_bounds__(PK_THREADS, N == 64 ? 2 : 1) k_packed_split(Pa
         decayed += cs[PK_Q - 1];
         for (int i = threadIdx.x; i < 64 * 32; i += PK_THREADS) {
             const int s = i >> 5, c = (i & 31) * 2;
-            const float w = wS[s];
+            const float w = wS[s], x0 = joined<PA>(Xs, s, c), x1 = joined<PA>(Xs, s, c + 1);
             uint32_t q[3];
-            split2(w * joined<PA>(Xs, s, c), w * joined<PA>(Xs, s, c + 1), q);
+            split2(AGAIN && isinf(x0) ? dts[s] * x0 : w * x0, AGAIN && isinf(x1) ? dts[s] * x1 : w * x1, q);
 #pragma unroll
             for (int k = 0; k < 3; ++k) *reinterpret_cast<uint32_t *>(&Ms[k].v[s][c]) = q[k];
         }
@@ -193,10 +201,16 @@ __global__ void __launch_bounds__(PK_THREADS, N == 64 ? 2 : 1) k_packed_split(Pa
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) hs[i].m[j][e] *= decay;
-            tile_mma<3, PA, true, true, false>(hs[i], Ms, Bs + i * PA);
+                for (int e = 0; e < 4; ++e)
+                    if (!AGAIN || !isinf(hs[i].m[j][e])) hs[i].m[j][e] *= decay;
+            tile_mma<3, PA, true, true, AGAIN>(hs[i], Ms, Bs + i * PA);
         }
         __syncthreads();                                  // the tiles are free
+    }
+    if constexpr (!AGAIN) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) nan |= hs[i].nan();
+        if (__syncthreads_or(nan)) return true;
     }
     if (SUMS) {
         entry += (u.range + 1) * HPN;
@@ -205,6 +219,16 @@ __global__ void __launch_bounds__(PK_THREADS, N == 64 ? 2 : 1) k_packed_split(Pa
     } else if (u.last && st && (u.n > 0 || !u.carry)) {
         each([&](int i, int j, int half, int at) { *reinterpret_cast<float2 *>(st + at) = hs[i].get(j, half); });
     }
+    return false;
+}
+
+template <int N, bool SUMS> __global__ void __launch_bounds__(PK_THREADS, N == 64 ? 2 : 1) k_packed_split(const __grid_constant__ PackedParams p) {
+    __shared__ ChunkVecs vecs;
+    pdl_launch_dependents();
+    pdl_wait();
+    // no wait of this kernel can run out: the status word is cleared, by the call's first launch
+    if ((SUMS || p.nsums == 0) && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = 0u;
+    if (packed_unit<N, SUMS, false>(p, vecs)) packed_unit<N, SUMS, true>(p, vecs);
 }
 
 }  // namespace
