@@ -301,7 +301,7 @@ typedef struct ssd_rows {
 /*
  * The scan of packed prompts.
  *   x, y [rows, H, P], Bm, Cm [rows, G, N] I/O dtype;  dt [rows, H], A, D [H] fp32, dt >= 0, A < 0
- *   y meets none of x, Bm, Cm (it may be other columns of the same wider tensor)
+ *   y meets none of x, dt, Bm, Cm, state (it may be other columns of the same wider tensor)
  *   state [nslots, H, P, N] fp32: the slots of the plan's sequences are read (carry) and replaced, the others left as they are
  *   ws    ssd_packed_workspace_bytes() bytes (0: bad arguments), 256-byte aligned
  * States and fp32 outputs are fp32 results in every dtype; cumulative sums of dt A are kept in 64 bits.  bf16 y: the masked scores and the
@@ -320,7 +320,7 @@ int ssd_packed_fwd(const ssd_rows_t *shape, const void *plan_host, const void *p
 /*
  * ssd_decode_step with states in slots: row b of x, dt, Bm, Cm, y belongs to slot slots[b] (DEVICE memory, read when the work runs; NULL:
  * slot b).  A row whose slot is negative or not below nslots is empty: nothing of it is read or written.  Where a slot is named more than
- * once, the first row has it and the others are empty.  rows <= 65535.  y meets none of x, Bm, Cm.
+ * once, the first row has it and the others are empty.  rows <= 65535.  y meets none of x, dt, Bm, Cm, state.
  */
 int ssd_decode_slots(const ssd_rows_t *shape, const void *x, const float *dt, const float *A, const void *Bm, const void *Cm, const float *D,
                      float *state, const int32_t *slots, void *y, void *stream);
@@ -330,7 +330,7 @@ int ssd_decode_slots(const ssd_rows_t *shape, const void *x, const float *dt, co
  * dense, multiples of 16 bytes) and for one token of each running sequence (slots as for ssd_decode_slots; 1 <= rows <= 65535).
  *   state [nslots, 3, C] I/O dtype, state_stride elements between slots (0 = 3 C; a multiple of 16 bytes): the last three inputs of a
  *         sequence, which the step moves on by one; sequences of fewer rows keep the rest of the old ones (carry) or zeros
- * out and u have no element in common (else SSD_EINVAL).  Return values as above.
+ * out has no element in common with u or state (else SSD_EINVAL).  Return values as above.
  */
 int ssd_conv_packed_fwd(const void *plan_host, const void *plan_dev, long long rows, int C, int dtype, const void *u, long long u_rstride,
                         const float *w, const float *bias, void *state, int nslots, long long state_stride, void *out, long long out_rstride,

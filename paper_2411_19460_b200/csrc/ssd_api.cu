@@ -1081,19 +1081,29 @@ static int rows_check(const ssd_rows_t *s, ssd_rows_t &r, int least) {
     return SSD_OK;
 }
 
-// Whether an output's rows and an input's have an element in common; both may be columns of one wider tensor
-static bool rows_meet(const void *out, int64_t out_rs, int64_t out_cols, const void *in, int64_t in_rs, int64_t in_cols, int64_t rows, int64_t e) {
+// Whether an output's rows and an input's have a byte in common; both may be columns of one wider tensor.  Strides and columns in bytes
+static bool rows_meet(const void *out, int64_t out_rs, int64_t out_cols, const void *in, int64_t in_rs, int64_t in_cols, int64_t rows) {
     if (rows == 0) return false;
     const int64_t a = (int64_t)(uintptr_t)out, b = (int64_t)(uintptr_t)in;
-    if (a >= b + ((rows - 1) * in_rs + in_cols) * e || b >= a + ((rows - 1) * out_rs + out_cols) * e) return false;
+    if (a >= b + (rows - 1) * in_rs + in_cols || b >= a + (rows - 1) * out_rs + out_cols) return false;
     if (out_rs != in_rs) return true;
-    const int64_t pitch = out_rs * e, off = ((b - a) % pitch + pitch) % pitch;          // of the input's columns behind the output's
-    return off < out_cols * e || off + in_cols * e > pitch;
+    const int64_t off = ((b - a) % out_rs + out_rs) % out_rs;          // of the input's columns behind the output's
+    return off < out_cols || off + in_cols > out_rs;
 }
-static bool y_meets(const ssd_rows_t &r, const void *y, const void *x, const void *Bm, const void *Cm) {
-    const int64_t HP = (int64_t)r.H * 64, GN = (int64_t)r.G * r.N, e = r.dtype == SSD_DTYPE_BF16 ? 2 : 4;
-    return rows_meet(y, r.y_rstride, HP, x, r.x_rstride, HP, r.rows, e) || rows_meet(y, r.y_rstride, HP, Bm, r.b_rstride, GN, r.rows, e) ||
-           rows_meet(y, r.y_rstride, HP, Cm, r.c_rstride, GN, r.rows, e);
+// Whether an output's rows reach into the slots of a cache (a slot's bytes), from the first to the last
+static bool rows_meet_slots(const void *out, int64_t out_rs, int64_t out_cols, int64_t rows, const void *state, int64_t stride, int64_t slot, int nslots) {
+    const int64_t a = (int64_t)(uintptr_t)out, b = (int64_t)(uintptr_t)state;
+    return rows && a < b + (nslots - 1) * stride + slot && b < a + (rows - 1) * out_rs + out_cols;
+}
+static bool y_meets(const ssd_rows_t &r, const void *y, const void *x, const float *dt, const void *Bm, const void *Cm, const float *state) {
+    const int64_t e = r.dtype == SSD_DTYPE_BF16 ? 2 : 4, HP = r.H * 64 * e, GN = (int64_t)r.G * r.N * e, rs = r.y_rstride * e;
+    return rows_meet(y, rs, HP, x, r.x_rstride * e, HP, r.rows) || rows_meet(y, rs, HP, Bm, r.b_rstride * e, GN, r.rows) ||
+           rows_meet(y, rs, HP, Cm, r.c_rstride * e, GN, r.rows) || rows_meet(y, rs, HP, dt, r.dt_rstride * 4, r.H * 4, r.rows) ||
+           rows_meet_slots(y, rs, HP, r.rows, state, r.state_stride * 4, (int64_t)r.H * 64 * r.N * 4, r.nslots);
+}
+static bool conv_out_meets(const void *out, int64_t out_rs, const void *u, int64_t u_rs, const void *state, int64_t stride, int nslots, int64_t rows, int C, int dtype) {
+    const int64_t e = dtype == SSD_DTYPE_BF16 ? 2 : 4;
+    return rows_meet(out, out_rs * e, C * e, u, u_rs * e, C * e, rows) || rows_meet_slots(out, out_rs * e, C * e, rows, state, stride * e, 3 * C * e, nslots);
 }
 
 static bool plan_fits(const PlanHeader *h, int64_t rows, int nslots) { return h && h->magic == kPlanMagic && h->rows <= rows && h->nslots <= nslots; }
@@ -1117,7 +1127,7 @@ int ssd_packed_fwd(const ssd_rows_t *shape, const void *plan_host, const void *p
         misaligned(state) || misaligned(y))
         return SSD_EALIGN;
     if (((uintptr_t)ws & 255u) || ws_bytes < ssd_packed_workspace_bytes(shape, plan_host)) return SSD_EWORKSPACE;
-    if (y_meets(r, y, x, Bm, Cm)) return SSD_EINVAL;
+    if (y_meets(r, y, x, dt, Bm, Cm, state)) return SSD_EINVAL;
     rc = check_device();
     if (rc) return rc;
     const int hpg = r.H / r.G;
@@ -1152,7 +1162,7 @@ int ssd_decode_slots(const ssd_rows_t *shape, const void *x, const float *dt, co
     if (misaligned(x) || ((uintptr_t)dt & 3) || ((uintptr_t)A & 3) || misaligned(Bm) || misaligned(Cm) || ((uintptr_t)D & 3) || misaligned(state) ||
         misaligned(y) || ((uintptr_t)slots & 3))
         return SSD_EALIGN;
-    if (y_meets(r, y, x, Bm, Cm)) return SSD_EINVAL;
+    if (y_meets(r, y, x, dt, Bm, Cm, state)) return SSD_EINVAL;
     rc = check_device();
     if (rc) return rc;
     SlotParams p = {r.rows, r.H, r.G, r.N, r.dtype, r.H / r.G, r.nslots, x, Bm, Cm, dt, A, D, y, state, slots,
@@ -1183,7 +1193,7 @@ int ssd_conv_packed_fwd(const void *plan_host, const void *plan_dev, long long r
     const PlanHeader *h = (const PlanHeader *)plan_host;
     if ((rows && (!u || !out)) || !plan_dev || !w || !bias || !state || !plan_fits(h, rows, nslots)) return SSD_EINVAL;
     if (misaligned(plan_dev) || misaligned(u) || misaligned(w) || misaligned(bias) || misaligned(state) || misaligned(out)) return SSD_EALIGN;
-    if (rows_meet(out, out_rstride, C, u, u_rstride, C, rows, dtype == SSD_DTYPE_BF16 ? 2 : 4)) return SSD_EINVAL;
+    if (conv_out_meets(out, out_rstride, u, u_rstride, state, state_stride, nslots, rows, C, dtype)) return SSD_EINVAL;
     rc = check_device();
     if (rc) return rc;
     cudaStream_t st = (cudaStream_t)stream;
@@ -1199,7 +1209,7 @@ int ssd_conv_step(long long rows, int C, int dtype, const void *u, long long u_r
     if (!u || !w || !bias || !state || !out || (!slots && rows > nslots)) return SSD_EINVAL;
     if (rows > 65535) return SSD_EUNSUPPORTED;
     if (misaligned(u) || misaligned(w) || misaligned(bias) || misaligned(state) || misaligned(out) || ((uintptr_t)slots & 3)) return SSD_EALIGN;
-    if (rows_meet(out, out_rstride, C, u, u_rstride, C, rows, dtype == SSD_DTYPE_BF16 ? 2 : 4)) return SSD_EINVAL;
+    if (conv_out_meets(out, out_rstride, u, u_rstride, state, state_stride, nslots, rows, C, dtype)) return SSD_EINVAL;
     rc = check_device();
     if (rc) return rc;
     cudaStream_t st = (cudaStream_t)stream;
