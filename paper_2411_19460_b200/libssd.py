@@ -388,10 +388,13 @@ class PackedPlan:
     constructor returns, and is kept until the calls on it are done."""
 
     def __init__(self, cu_seqlens, *, slots=None, carry=None, nslots=None, heads, device="cuda"):
-        cu = torch.as_tensor(cu_seqlens, dtype=torch.int64, device="cpu").contiguous()
+        cu = torch.as_tensor(cu_seqlens, device="cpu")
         n = cu.numel() - 1
         if cu.dim() != 1 or n < 1:
             raise ValueError("cu_seqlens must have one entry more than there are sequences")
+        if bool((cu.to(torch.int64) != cu).any()):
+            raise ValueError("cu_seqlens must be whole numbers")
+        cu = cu.to(torch.int64).contiguous()
         per_seq = []
         for name, v in (("slots", slots), ("carry", carry)):
             if v is not None:
