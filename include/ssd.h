@@ -279,7 +279,8 @@ int ssd_gated_norm_bwd(long long rows, int D, int group, int dtype, const void *
  *   plan        HOST buffer of ssd_plan_bytes() bytes (0: bad arguments), 16-byte aligned.  Calls take it twice: as it is (plan_host, read
  *               before return) and as the caller's copy in device memory (plan_dev, the same bytes, 16-byte aligned), which has to stay
  *               until the work is done.
- * ssd_plan_make returns SSD_OK, SSD_EINVAL, SSD_EALIGN or SSD_EWORKSPACE (plan too small).
+ * ssd_plan_make returns SSD_OK, SSD_EINVAL, SSD_EALIGN or SSD_EWORKSPACE (plan too small).  Both calls choose how sequences are cut, by the estimated
+ * times of up to 21 ways: 0.1 ms of host time for a short prompt, 5 for 24 of some thousand rows and 80 heads, 15 for 512 of them.
  */
 size_t ssd_plan_bytes(int nseq, const int64_t *cu_seqlens, int heads);
 int ssd_plan_make(int nseq, const int64_t *cu_seqlens, const int32_t *slots, const int32_t *carry, int nslots, int heads, void *plan,

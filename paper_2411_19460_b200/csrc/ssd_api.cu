@@ -928,7 +928,10 @@ bool heads_by_twos(int64_t units, int heads) { return units * heads > kNumSMs; }
 //   three of 4096 rows, 80 heads    168   168   168      30 of 100 to 6000, 32 heads  400   400   400
 //   one of 16384 rows, 24 heads, N = 64   302   104   102
 // fp32 takes ten times as long in much the same proportions (one of 16384 rows, 24 heads 3191, 750, 750), but for short sequences, where a CTA's
-// start weighs less: seven of 17 to 510 rows of 4 heads 106, 106, 43.  A plan does not know the type.
+// start weighs less: seven of 17 to 510 rows of 4 heads 106, 106, 43.  A plan does not know the type,
+// the state size or the groups: fp32 and groups of one head have a head per CTA where this counts two.
+// Host time of a plan, most of it here (ssd_plan_bytes and ssd_plan_make choose both): one prompt of 37 rows 0.1 ms, seven of up to 1500 rows of 24
+// heads 0.3, 24 of up to 4000 of 80 heads 5, one of 49153 of 64 heads 2.4, 512 of up to 8000 of 80 heads 15 (one core, once for all layers).
 int ranges_of(int64_t n, int rows) { return n > rows ? (int)((n + rows - 1) / rows) : 1; }
 // rows of range r of m of a sequence of n: equal parts in blocks
 void range_at(int64_t n, int m, int r, int64_t &begin, int64_t &end) {
@@ -1000,7 +1003,9 @@ bool plan_sizes(int nseq, const int64_t *cu, int heads, PlanSizes &s) {
     } catch (...) {
         s.rows = INT32_MAX;
     }
-    // short tiles where there are few: their three rows in front cost less than SMs without work
+    // Short tiles where there are few: their three rows in front cost less than SMs without work.  us with 8, 16, 32, 64 rows of 1792 channels in bf16 (of
+    // 5376): 700 rows 6.5, 6.9, 7.0, 11.1 (7.2, 9.4, 12.9, 15.1); 2000 7.3, 9.4, 12.6, 11.1 (13.6, 12.2, 15.1, 24.3); 4096 10.9, 10.0, 14.6, 22.0 (25.8, 19.8,
+    // 20.2, 26.5); 16384 37.6, 29.3, 27.6, 27.9 (101, 74.6, 64.3, 64.1); 60000 134, 96, 82, 81 (377, 265, 220, 218); fp32 lies between.
     s.tile = cu[nseq] <= 1024 ? 8 : cu[nseq] <= 4096 ? 16 : cu[nseq] <= 16384 ? 32 : kConvTile;
     for (int i = 0; i < nseq; ++i) {
         const int64_t n = cu[i + 1] - cu[i];

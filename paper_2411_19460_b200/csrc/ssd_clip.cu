@@ -3,11 +3,12 @@
 // The factor is fp32.  A norm above fp32's largest value, or a factor below its smallest normal one, which would have few bits left, are kept in 64
 // bits, and the gradients then multiplied so, one by one.
 // Two launches.  The first walks all tensors in chunks, a number of CTAs that the sizes fix, and leaves one sum per CTA in 64 bits;
-// in the second every CTA adds those sums up in the same order and scales its chunks, the last read first, which the L2 cache still
-// holds.  Squares of up to 16 elements are added in 32 bits, everything above in 64; those whose sum leaves the middle of the range (below
-// 1e-30, where squares are lost, or above 1e30, infinities and NaN among them) are taken again in 64 bits.
-// Bound by memory: 483 MB of gradients 241 us, two readings and a writing at 6.0 TB/s (75 us the norm, at 6.4).  384 small vectors take 18 us
-// on the device, 24 with the host's part of the call, which is the longer one.
+// in the second every CTA adds those sums up in the same order and scales its chunks, the last read first (of small gradients the
+// L2 cache has all; of 483 MB it keeps nothing: the second reading takes all of them from memory again).  Squares of up to 16
+// elements are added in 32 bits, everything above in 64; those whose sum leaves the middle of the range (below 1e-30, where squares
+// are lost, or above 1e30, infinities and NaN among them) are taken again in 64 bits.
+// Bound by memory: 483 MB of gradients 240 us, two readings and a writing at 6.0 TB/s (74 us the norm, at 6.5).  384 small vectors take
+// 16 us on the device, 25 with the host's part of the call, which is the longer one.
 // The table of tensors travels in the launch's parameters: no copy to the device, and a captured graph has it by value.
 #include <cfloat>
 

@@ -22,13 +22,14 @@
 // Warps, meeting only through mbarriers (tests/test_packed_halves.py and test_packed_roles.py have a model of who waits for what):
 //   0 G and M X   1 S and C H   2, 3 decays of even and odd items   4..11 parts of x'   12..15 outputs   16..23 mask, but for one without
 //   a sub-tile: loads   24..31 states, half of p each four
-// Bound by shared memory: 4150 cycles an item (two heads), in which the products' operands take 2430 at 128 bytes a cycle, the parts of x' 510, the
-// states' 260, outputs 260 and the copies in and out 500, and the tensor pipe 2690.  24 prompts, 23760 tokens, of 80 heads: 342 us (1.8 TB/s; its bytes
-// alone 93 us), three of 4096 168 us, one of 49153 of 64 heads with 8 groups 786 with its sums (a pass among others).  What it took: y over x and parts of x'
-// in a ring of three times 32 steps instead of twice 64, and x ahead of C; factors of the mask from the middle row (for strong decays); short code, for
-// the roles' loops together go through the instruction cache once per item; with two parts of M and H, C H in two places and the halves of M one by one (353
-// -> 342).  Four items' x instead of three made no difference.  Taken back, slower or no faster: scores ahead of M X, or what of the two is ready first;
-// C H behind the next item's S; y by warps; the next block prefetched into L2; polls that sleep or stay; sums given back ahead of the last stores.
+// Bound by shared memory: of 4150 cycles an item (two heads; 2.5 us at 1.65 GHz) the products' operands take 2430 at 128 bytes a cycle, by count, and loads
+// and stores of threads keep its pipe busy for 1700 (41% of all cycles, by counter); the tensor pipe works for 2690.  24 prompts, 23760 tokens, of 80 heads:
+// 342 us (1.8 TB/s; its bytes alone 93 us), three of 4096 168 us, one of 49153 of 64 heads with 8 groups 786, 245 of them for its sums (a pass among
+// others).  What it took: y over x and parts of x' in a ring of three times 32 steps instead of twice 64, and x ahead of C; factors of the mask from the middle
+// row (for strong decays); short code, for the roles' loops together go through the instruction cache once per item; with two parts of M and H, C H in two
+// places and the halves of M one by one (353 -> 342).  Four items' x instead of three make no difference, for the sums either.  Taken back, slower or
+// no faster: scores ahead of M X, or what of the two is ready first; C H behind the next item's S; y by warps; the next block prefetched into L2; polls that
+// sleep or stay; sums given back ahead of the last stores.
 #include "ssd_internal.h"
 #include "ssd_packed.h"
 #include "ssd_split.cuh"
