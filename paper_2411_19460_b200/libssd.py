@@ -236,12 +236,14 @@ def _check_inputs(x, dt, A, Bm, Cm, D):
         raise TypeError("Bm, Cm must have the dtype of x")
 
 
-def _of_stream(stream, make):
-    """A dict of new tensors in memory of a call's stream (as CallStream in csrc/binding.cpp has it)."""
-    now = torch.cuda.current_stream()
-    if stream is None or stream.cuda_stream == now.cuda_stream:
+def _of_stream(stream, dev, make):
+    """A dict of new tensors on `dev` in memory of a call's stream (as CallStream in csrc/binding.cpp has it)."""
+    if stream is None or dev.type != "cuda":
         return make()
-    with torch.cuda.stream(torch.cuda.ExternalStream(stream.cuda_stream) if stream.cuda_stream else torch.cuda.default_stream()):
+    now, at = torch.cuda.current_stream(dev), stream.cuda_stream
+    if at == now.cuda_stream:
+        return make()
+    with torch.cuda.stream(torch.cuda.ExternalStream(at, device=dev) if at else torch.cuda.default_stream(dev)):
         out = make()
     for t in out.values():
         if t is not None:
@@ -289,7 +291,7 @@ def ssd_bwd_segmented(x, dt, A, Bm, Cm, D, boundary, dy, dh_final=None, *, chunk
     if out is None:
         B, _, H, P = x.shape
         N, dev = Bm.shape[3], x.device
-        out = _of_stream(stream, lambda: dict(
+        out = _of_stream(stream, dev, lambda: dict(
             dx=torch.empty_like(x), ddt=torch.empty_like(dt), dA=torch.empty(H, dtype=torch.float32, device=dev),
             dB=torch.empty_like(Bm), dC=torch.empty_like(Cm), dD=torch.empty(H, dtype=torch.float32, device=dev),
             dh0=torch.empty(B, H, P, N, dtype=torch.float32, device=dev) if want_dh0 else None))

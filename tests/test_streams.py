@@ -176,3 +176,23 @@ def test_a_captured_call_on_a_stream_of_its_own():
         t["state"].copy_(before)
         graph.replay()
         assert torch.equal(got, y) and torch.equal(t["state"], after)
+
+
+@pytest.mark.gpu
+def test_the_default_stream_given_while_another_is_current():
+    t = make([512], 4, 1, 128, "bf16", seed=59)
+    args = [t[k].contiguous()[None] if t[k].dim() > 1 else t[k] for k in ("x", "dt", "A", "Bm", "Cm", "D")]
+    y, _, boundary = libssd.ssd_fwd_segmented(*args, t["state"], chunk=256, seg=256)
+    ref = libssd.ssd_bwd_segmented(*args, boundary, y, chunk=256, seg=256)
+    grads = [torch.randn(5000, device="cuda")]
+    out = [torch.empty_like(grads[0])]
+    norm = float(libssd.ssd_grad_clip(grads, 1.0, out=out))
+    torch.cuda.synchronize()
+    default = torch.cuda.default_stream()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        got = libssd.ssd_bwd_segmented(*args, boundary, y, chunk=256, seg=256, stream=default)
+        first = libssd.ssd_fwd(*args, t["state"], chunk=256, seg=256, stream=default)[0]
+        clipped = libssd.ssd_grad_clip(grads, 1.0, stream=default)
+    torch.cuda.synchronize()
+    assert all(torch.equal(got[k], ref[k]) for k in ref) and torch.equal(first, y)
+    assert float(clipped) == norm and torch.equal(grads[0], out[0])
