@@ -12,7 +12,7 @@
 //
 // What is rounded: X' to three bf16 parts (nothing is lost: the states are fp32 results).  M and H to two, 2^-16 of each of their terms in y, which
 // is itself rounded to 2^-8; D x is added in fp32.  One part of each, 2^-8 of its terms, costs y 40% more error than its own rounding where the products
-// are all of it (D = 0), and nothing where D x is most of it: 24 prompts took 305 us so, the second part of M 26 more, that of H 22 (now 342).
+// are all of it (D = 0), and nothing where D x is most of it: 24 prompts took 305 us so, the second part of M 26 more, that of H 22.
 // Sums are fp32 in tensor memory.  cs is summed in 64 bits and kept as two fp32 numbers: with strong decays it runs into the thousands.
 //
 // Products (cycles of the tensor pipe): G 512 a block; S 1150 (one part after the other onto the same sums, N = 64, which 48 cycles of reading
@@ -22,14 +22,15 @@
 // Warps, meeting only through mbarriers (tests/test_packed_halves.py and test_packed_roles.py have a model of who waits for what):
 //   0 G and M X   1 S and C H   2, 3 decays of even and odd items   4..11 parts of x'   12..15 outputs   16..23 mask, but for one without
 //   a sub-tile: loads   24..31 states, half of p each four
-// Bound by shared memory: of 4150 cycles an item (two heads; 2.5 us at 1.65 GHz) the products' operands take 2430 at 128 bytes a cycle, by count, and loads
-// and stores of threads keep its pipe busy for 1700 (41% of all cycles, by counter); the tensor pipe works for 2690.  24 prompts, 23760 tokens, of 80 heads:
-// 342 us (1.8 TB/s; its bytes alone 93 us), three of 4096 168 us, one of 49153 of 64 heads with 8 groups 786, 245 of them for its sums (a pass among
-// others).  What it took: y over x and parts of x' in a ring of three times 32 steps instead of twice 64, and x ahead of C; factors of the mask from the middle
-// row (for strong decays); short code, for the roles' loops together go through the instruction cache once per item; with two parts of M and H, C H in two
-// places and the halves of M one by one (353 -> 342).  Four items' x instead of three make no difference, for the sums either.  Taken back, slower or
-// no faster: scores ahead of M X, or what of the two is ready first; C H behind the next item's S; y by warps; the next block prefetched into L2; polls that
-// sleep or stay; sums given back ahead of the last stores.
+// Bound by shared memory and the hand-overs between the roles: of 4150 cycles an item (two heads; 2.5 us at 1.65 GHz) the products' operands take 2430 at 128
+// bytes a cycle, by count, loads and stores of threads keep its pipe busy for 1700 (41% of all cycles, by counter), and the tensor pipe works for 2690.
+// 24 prompts, 23760 tokens, of 80 heads: 345 us (1.7 TB/s; its bytes alone 93 us), three of 4096 168 us, one of 49153 of 64 heads with 8 groups 800, 245 of
+// them for its sums (a pass among others).  What it took: y over x and parts of x' in a ring of three times 32 steps instead of twice 64, and x ahead of
+// C; factors of the mask from the middle row (for strong decays); short code, for the roles' loops together go through the instruction cache once per
+// item; with two parts of M and H, C H in two places and the halves of M one by one (353 -> 343).  Four items' x instead of three make no difference,
+// for the sums either.  Taken back, slower or no faster: scores ahead of M X, or what of the two is ready first; C H behind the next item's S; y by
+// warps; the next block prefetched into L2; polls that sleep or stay; sums given back ahead of the last stores; C H of both parts of H side by side, N =
+// 128, which reads C once but has one place (352).
 #include "ssd_internal.h"
 #include "ssd_packed.h"
 #include "ssd_split.cuh"
